@@ -328,6 +328,154 @@ tf_status_t treeflash_accept(const int32_t *node_token, const int32_t *node_pare
                              int b, int B, int gamma, int32_t *accepted, int32_t *accept_len,
                              int32_t *bonus, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The verification step beside the tree: a next token for every position
+ * (treeflash_sample, whose tokens are treeflash_accept's `target`), cache
+ * pages and slots for the accepted path (treeflash_cache_slots), its keys and
+ * values into a paged 8-bit cache (treeflash_cache_append) and attention of a
+ * tree's positions over that cache (treeflash_tree_attention).
+ *
+ * The cache of one layer:
+ *   k_cache  [num_pages, Hkv, page_size, D]  e4m3 (OCP, 448 the largest value)
+ *   v_cache  [num_pages, Hkv, D, page_size]  e4m3, a page's values transposed
+ *   k_scale, v_scale  [num_pages, Hkv] fp32  a stored code times its page's
+ *            and head's scale is the value; scales are powers of two in
+ *            2^-64..2^64
+ *   block_table [b, max_pages] int32: page of tokens p*page_size.. of a sequence
+ * page_size is 16, 32, 64 or 128 and D 64 or 128, else TF_ERR_UNSUPPORTED.
+ * A tree's own keys and values are not in the cache: the attention reads them
+ * from k_new and v_new, and only the accepted path is appended afterwards. */
+
+/* Workspace bytes of treeflash_sample; 0 for invalid shapes.  A larger b or n
+ * never needs less. */
+size_t treeflash_sample_workspace_bytes(int b, int n, int V);
+
+/* A token for each of n positions of b sequences, from given random numbers.
+ *   logits       rows of V values (dtype dt); row r = s*n + i starts at element r*ld,
+ *                ld >= V (any alignment of the element size)
+ *   temperature  [b] fp32 or NULL (1): 0 (or below, or NaN) takes the largest logit
+ *   top_k        [b] int32 or NULL: <= 0 or >= V is off
+ *   top_p        [b] fp32 or NULL: >= 1 or NaN is off
+ *   min_p        [b] fp32 or NULL: <= 0 or NaN is off
+ *   uniform      [b, n] fp32 in [0, 1) (clamped to it; NaN counts as 0)
+ *   token        out [b, n] int32
+ *   logprob      out [b, n] fp32 or NULL: log of the token's probability among
+ *                the kept ones
+ * w_v = exp((z_v - max z) / temperature).  Tokens rank by (z desc, id asc);
+ * kept are the first top_k of them, of these the shortest prefix that holds
+ * top_p of their mass, and of these the ones with w_v >= min_p (the first
+ * token always stays).  The token is the first one, by id, at which the
+ * running sum of the kept w exceeds uniform times their total.  Weights and
+ * sums are exact to about 2^-44 of the largest weight, whatever the order of
+ * the additions, so a result does not depend on the launch.
+ * NaN counts as -inf, and -inf is never drawn: a row of them alone gives token
+ * -1 and logprob -inf.  Where +inf occurs its tokens share the whole mass.
+ * V <= 2^22. */
+tf_status_t treeflash_sample(const void *logits, long long ld, int b, int n, int V, tf_dtype_t dt,
+                             const float *temperature, const int32_t *top_k, const float *top_p,
+                             const float *min_p, const float *uniform, int32_t *token, float *logprob,
+                             void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Pages, slots and positions of the tokens that b sequences gain.  Needs no
+ * workspace.
+ *   context_len  [b] int32 tokens held before
+ *   add_len      [b] int32 tokens gained; with `accepted`, the accept_len of
+ *                treeflash_accept, and the sequence gains 1 + add_len tokens:
+ *                the root and its accepted nodes
+ *   accepted     [b, gamma] int32 of treeflash_accept, or NULL (gamma unused)
+ *   n            positions a sequence has in the arrays of new keys and values
+ *                (B + 1 with `accepted`), or 0 where their rows are packed
+ *   free_pages   [max_free] int32 and free_count [1]: a stack of free pages;
+ *                pages are taken from its end, in sequence order
+ *   block_table  in/out [b, max_pages]: entries of the pages taken are written
+ *   new_len      out [b] (may be context_len itself)
+ *   new_free_count out [1] (may be free_count itself)
+ *   start        out [b+1]: first of each sequence's tokens in the lists below
+ *   page_start   out [b+1]: pages taken by the sequences before
+ *   slot         out [max_tokens]: page * page_size + offset in the page
+ *   position     out [max_tokens] or NULL: position in the sequence
+ *   source       out [max_tokens] or NULL: row of the new keys and values,
+ *                s*n + (0 for the root, 1 + node for accepted ones, j without
+ *                `accepted`), or the token's own index where n is 0
+ *   status       out [1]: 0, or why nothing was taken -- 1: a negative or
+ *                impossible length, 2: more than max_tokens tokens, 3: a
+ *                sequence outgrows its table, 4: too few free pages
+ * Behind the last token the three lists read -1.  With a status other than 0
+ * lengths, count and table stay, start and page_start read 0 and the lists -1.
+ * slot fits 32 bits as long as num_pages * page_size <= 2^31. */
+tf_status_t treeflash_cache_slots(const int32_t *context_len, const int32_t *add_len, const int32_t *accepted,
+                                  const int32_t *free_pages, const int32_t *free_count, int b, int gamma, int n,
+                                  int page_size, int max_pages, int max_free, int max_tokens,
+                                  int32_t *block_table, int32_t *new_len, int32_t *new_free_count,
+                                  int32_t *start, int32_t *page_start, int32_t *slot, int32_t *position,
+                                  int32_t *source, int32_t *status, hipStream_t stream);
+
+/* Gives the pages of finished sequences back: those of every sequence with
+ * done[s] != 0 are pushed onto the stack, in order, and its length becomes 0.
+ *   done         [b] uint8
+ *   new_len, new_free_count  out, may be context_len and free_count themselves
+ * Pages past the stack's max_free entries are dropped. */
+tf_status_t treeflash_cache_release(const uint8_t *done, const int32_t *context_len, const int32_t *block_table,
+                                    const int32_t *free_count, int b, int page_size, int max_pages, int max_free,
+                                    int32_t *free_pages, int32_t *new_len, int32_t *new_free_count,
+                                    hipStream_t stream);
+
+/* Writes keys and values into the cache.  Needs no workspace.
+ *   k_new, v_new  rows of [Hkv, D] (dtype dt), row r at element r*ld_new;
+ *                 16-byte aligned, ld_new*element size a multiple of 16
+ *   slot          [N] int32; a slot outside the cache (-1) writes nothing
+ *   source        [N] int32 or NULL (row i): row that goes to slot i; a row
+ *                 outside 0..rows-1 stores zeros
+ * The tokens of a page are a run of consecutive slots in the list, appended in
+ * order behind what the page holds: a run that begins at offset o > 0 keeps the
+ * page's first o tokens.  The scale of a page and head is the smallest power of
+ * two that brings its values into +-448 and never falls while the page fills;
+ * where it rises, the o tokens are rounded again.  Codes are rounded to nearest
+ * even, infinities stored as +-448 and NaN as NaN, neither entering the scale.
+ * Bytes of a page behind the run stay as they were.  Two runs of one list in
+ * the same page give unspecified values. */
+tf_status_t treeflash_cache_append(const void *k_new, const void *v_new, long long ld_new, int rows,
+                                   const int32_t *slot, const int32_t *source, int N, int Hkv, int D,
+                                   int page_size, int num_pages, tf_dtype_t dt, void *k_cache, void *v_cache,
+                                   float *k_scale, float *v_scale, hipStream_t stream);
+
+/* Workspace bytes of treeflash_tree_attention; 0 for invalid shapes.  Few
+ * sequences are split into more parts, so a smaller b or n can need more: ask
+ * for the shapes of each call. */
+size_t treeflash_tree_attention_workspace_bytes(int b, int n, int Hq, int Hkv, int D, int page_size,
+                                                int max_pages, tf_dtype_t dt);
+
+/* Attention of n new positions of each sequence over its cached context and
+ * over the new positions themselves.
+ *   q            rows of [Hq, D] (dtype dt), position i of sequence s at element
+ *                (s*n + i)*ld_q; Hq a multiple of Hkv, head h reads key head
+ *                h / (Hq / Hkv)
+ *   k_new, v_new rows of [Hkv, D], position i of s at element (s*n + i)*ld_new
+ *   mask         [b, n, n] uint8 (treeflash_tree_attention_inputs): position i
+ *                attends to new position j where mask[s][i][j] != 0; NULL: j <= i
+ *   new_len      [b] int32 or NULL (n): positions that sequence s really has;
+ *                outputs of the others stay as they were
+ *   context_len  [b] int32 tokens in the cache (held to 0..max_pages*page_size)
+ *   scale        factor of q.k before the softmax, finite
+ *   out          [b, n, Hq, D] dense, dtype dt
+ *   lse          out [b, n, Hq] fp32 log-sum-exp of the scaled products, or NULL
+ * A context token whose table entry is no page of the cache is not attended
+ * to; a position that attends to nothing reads 0 and lse -inf.  What lies
+ * behind a sequence's tokens in a page, and keys and values that the mask
+ * excludes, may be anything.  q, k_new, v_new, both caches and out are 16-byte
+ * aligned, ld_q and ld_new times the element size multiples of 16.
+ * bf16 multiplies bf16 queries with the stored codes and fp16 softmax weights
+ * with the cached values (both exact in their 8-bit operand), sums in fp32;
+ * TF_F32 works in fp32 throughout.  n <= 4096. */
+tf_status_t treeflash_tree_attention(const void *q, long long ld_q, const void *k_new, const void *v_new,
+                                     long long ld_new, const uint8_t *mask, const int32_t *new_len,
+                                     const int32_t *context_len, const int32_t *block_table,
+                                     const void *k_cache, const void *v_cache, const float *k_scale,
+                                     const float *v_scale, int b, int n, int Hq, int Hkv, int D,
+                                     int page_size, int max_pages, int num_pages, float scale,
+                                     tf_dtype_t dt, void *out, float *lse, void *workspace,
+                                     size_t workspace_bytes, hipStream_t stream);
+
 /* Static description of a status code. */
 const char *treeflash_status_string(tf_status_t status);
 

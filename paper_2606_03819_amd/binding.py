@@ -25,6 +25,8 @@ EXPORTED = ("treeflash_workspace_bytes", "treeflash_marginal_topk", "treeflash_m
             "treeflash_build_tree",
             "treeflash_build_tree_marginal", "treeflash_tree_attention_inputs", "treeflash_accept",
             "treeflash_workspace_bytes_2prev", "treeflash_arapprox_2prev_hidden", "treeflash_build_tree_2prev",
+            "treeflash_sample_workspace_bytes", "treeflash_sample", "treeflash_cache_slots", "treeflash_cache_release",
+            "treeflash_cache_append", "treeflash_tree_attention_workspace_bytes", "treeflash_tree_attention",
             "treeflash_status_string")
 
 _lib = None
@@ -76,6 +78,21 @@ def lib() -> ctypes.CDLL:
     L.treeflash_arapprox_2prev_hidden.restype = I
     L.treeflash_build_tree_2prev.argtypes = [P, P, P, I, I, I, I, I, P, P, P, P, P, P]
     L.treeflash_build_tree_2prev.restype = I
+    LL = ctypes.c_longlong
+    L.treeflash_sample_workspace_bytes.argtypes = [I, I, I]
+    L.treeflash_sample_workspace_bytes.restype = S
+    L.treeflash_sample.argtypes = [P, LL, I, I, I, I, P, P, P, P, P, P, P, P, S, P]
+    L.treeflash_sample.restype = I
+    L.treeflash_cache_slots.argtypes = [P] * 5 + [I] * 7 + [P] * 10
+    L.treeflash_cache_slots.restype = I
+    L.treeflash_cache_release.argtypes = [P] * 4 + [I] * 4 + [P] * 4
+    L.treeflash_cache_release.restype = I
+    L.treeflash_cache_append.argtypes = [P, P, LL, I, P, P, I, I, I, I, I, I, P, P, P, P, P]
+    L.treeflash_cache_append.restype = I
+    L.treeflash_tree_attention_workspace_bytes.argtypes = [I] * 8
+    L.treeflash_tree_attention_workspace_bytes.restype = S
+    L.treeflash_tree_attention.argtypes = [P, LL, P, P, LL] + [P] * 8 + [I] * 8 + [F, I] + [P, P, P, S, P]
+    L.treeflash_tree_attention.restype = I
     L.treeflash_status_string.argtypes = [I]
     L.treeflash_status_string.restype = ctypes.c_char_p
     _lib = L
@@ -415,6 +432,201 @@ def treeflash_accept(tree: Dict[str, torch.Tensor], target: torch.Tensor, gamma:
         _ptr(out["bonus"], "bonus", torch.int32, dev), _stream(dev))
     _check("treeflash_accept", st)
     return out
+
+
+# ---------------------------------------------------- the verification step beside the tree
+
+E4M3 = torch.float8_e4m3fn
+
+
+def _launch(func: str, dev, *args):
+    """Calls the library with `dev` the current device (its streams belong to it) and `dev`'s current stream."""
+    f = getattr(lib(), func)
+    if dev.index is None or torch.cuda.current_device() == dev.index:
+        _check(func, f(*args, _stream(dev)))
+    else:
+        with torch.cuda.device(dev):
+            _check(func, f(*args, _stream(dev)))
+
+
+def _rows_ptr(t: torch.Tensor, name: str, inner: int, dtype, device) -> tuple:
+    """Pointer and row distance (elements) of a tensor whose last `inner` dimensions are dense and whose
+    leading ones step evenly from row to row."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    width = 1
+    for size, stride in zip(reversed(t.shape[-inner:]), reversed(t.stride()[-inner:])):
+        if size != 1 and stride != width:
+            raise ValueError(f"{name} must be dense in its last {inner} dimension(s)")
+        width *= size
+    lead = [(size, stride) for size, stride in zip(t.shape[:-inner], t.stride()[:-inner]) if size != 1]
+    ld = lead[-1][1] if lead else width
+    want = ld
+    for size, stride in reversed(lead):
+        if stride != want:
+            raise ValueError(f"{name}: rows must lie at one distance")
+        want = stride * size
+    return t.data_ptr(), ld
+
+
+def treeflash_sample_workspace_bytes(b: int, n: int, V: int) -> int:
+    return int(lib().treeflash_sample_workspace_bytes(b, n, V))
+
+
+def treeflash_sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                     top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                     min_p: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     token: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None):
+    """A token for every position from logits [b, n, V] (rows may be padded) and random numbers uniform [b, n]
+    in [0, 1); temperature, top_k, top_p and min_p are [b] or None (off).  Returns token [b, n] int32, which is
+    treeflash_accept's target, and its log-probability among the kept tokens [b, n]."""
+    b, n, V = logits.shape
+    dev = logits.device
+    _shapes("treeflash_sample", uniform=(uniform, (b, n)), temperature=(temperature, (b,)), top_k=(top_k, (b,)),
+            top_p=(top_p, (b,)), min_p=(min_p, (b,)), token=(token, (b, n)), logprob=(logprob, (b, n)))
+    dt = _dtype_code(logits)
+    ptr, ld = _rows_ptr(logits, "logits", 1, logits.dtype, dev)
+    if token is None:
+        token = torch.empty((b, n), dtype=torch.int32, device=dev)
+    if logprob is None:
+        logprob = torch.empty((b, n), dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = alloc_workspace(treeflash_sample_workspace_bytes(b, n, V), dev)
+    f32 = torch.float32
+    _launch("treeflash_sample", dev, ptr, ld, b, n, V, dt, _ptr(temperature, "temperature", f32, dev),
+            _ptr(top_k, "top_k", torch.int32, dev), _ptr(top_p, "top_p", f32, dev), _ptr(min_p, "min_p", f32, dev),
+            _ptr(uniform, "uniform", f32, dev), _ptr(token, "token", torch.int32, dev),
+            _ptr(logprob, "logprob", f32, dev), _ptr(workspace, "workspace", device=dev),
+            workspace.numel() * workspace.element_size())
+    return token, logprob
+
+
+def treeflash_cache_slots(context_len: torch.Tensor, add_len: torch.Tensor, free_pages: torch.Tensor,
+                          free_count: torch.Tensor, block_table: torch.Tensor, page_size: int, max_tokens: int,
+                          accepted: Optional[torch.Tensor] = None, n: int = 0, out: Optional[dict] = None):
+    """Pages, slots and positions of the tokens that each sequence gains, from lengths on the GPU: add_len [b]
+    tokens, or with `accepted` [b, gamma] (treeflash_accept's, add_len its accept_len) the root and the accepted
+    nodes of a tree input of n positions.  block_table is updated in place.  `out` may hold context_len and
+    free_count themselves to update them in place; status 0 says that the pages sufficed."""
+    b, max_pages = block_table.shape
+    dev = block_table.device
+    i32 = torch.int32
+    gamma = accepted.shape[1] if accepted is not None else 0
+    if out is None:
+        e = dict(dtype=i32, device=dev)
+        out = {"context_len": torch.empty((b,), **e), "free_count": torch.empty((1,), **e),
+               "start": torch.empty((b + 1,), **e), "page_start": torch.empty((b + 1,), **e),
+               "slot": torch.empty((max_tokens,), **e), "position": torch.empty((max_tokens,), **e),
+               "source": torch.empty((max_tokens,), **e), "status": torch.empty((1,), **e)}
+    out["block_table"] = block_table
+    _shapes("treeflash_cache_slots", context_len=(context_len, (b,)), add_len=(add_len, (b,)),
+            accepted=(accepted, (b, gamma)), free_pages=(free_pages, (free_pages.numel(),)),
+            free_count=(free_count, (1,)), new_len=(out["context_len"], (b,)), new_count=(out["free_count"], (1,)),
+            start=(out["start"], (b + 1,)), page_start=(out["page_start"], (b + 1,)),
+            slot=(out["slot"], (max_tokens,)), position=(out.get("position"), (max_tokens,)),
+            source=(out.get("source"), (max_tokens,)), status=(out["status"], (1,)))
+    _launch("treeflash_cache_slots", dev, _ptr(context_len, "context_len", i32, dev), _ptr(add_len, "add_len", i32, dev),
+            _ptr(accepted, "accepted", i32, dev), _ptr(free_pages, "free_pages", i32, dev),
+            _ptr(free_count, "free_count", i32, dev), b, gamma, n, page_size, max_pages, free_pages.numel(), max_tokens,
+            _ptr(block_table, "block_table", i32, dev),
+            *[_ptr(out.get(f), f, i32, dev) for f in ("context_len", "free_count", "start", "page_start", "slot",
+                                                      "position", "source", "status")])
+    return out
+
+
+def treeflash_cache_release(done: torch.Tensor, context_len: torch.Tensor, block_table: torch.Tensor,
+                            free_pages: torch.Tensor, free_count: torch.Tensor, page_size: int):
+    """Gives the pages of the sequences with done [b] (uint8) back; lengths, stack and count change in place."""
+    b, max_pages = block_table.shape
+    dev = block_table.device
+    i32 = torch.int32
+    _shapes("treeflash_cache_release", done=(done, (b,)), context_len=(context_len, (b,)),
+            free_pages=(free_pages, (free_pages.numel(),)), free_count=(free_count, (1,)))
+    ln, fc = _ptr(context_len, "context_len", i32, dev), _ptr(free_count, "free_count", i32, dev)
+    _launch("treeflash_cache_release", dev, _ptr(done, "done", torch.uint8, dev), ln,
+            _ptr(block_table, "block_table", i32, dev), fc, b, page_size, max_pages, free_pages.numel(),
+            _ptr(free_pages, "free_pages", i32, dev), ln, fc)
+
+
+def _cache_shapes(func: str, k_cache, v_cache, k_scale, v_scale, Hkv: int, D: int):
+    num_pages, _, page_size, _ = k_cache.shape
+    _shapes(func, k_cache=(k_cache, (num_pages, Hkv, page_size, D)), v_cache=(v_cache, (num_pages, Hkv, D, page_size)),
+            k_scale=(k_scale, (num_pages, Hkv)), v_scale=(v_scale, (num_pages, Hkv)))
+    return num_pages, page_size
+
+
+def treeflash_cache_append(k_new: torch.Tensor, v_new: torch.Tensor, slot: torch.Tensor, k_cache: torch.Tensor,
+                           v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                           source: Optional[torch.Tensor] = None):
+    """Writes keys and values [..., Hkv, D] into the cache: row source[i] (None: i) to slot[i], -1 none.  The
+    rows may be views of a wider projection.  Caches are float8_e4m3fn, k [pages, Hkv, page_size, D], v
+    [pages, Hkv, D, page_size], scales [pages, Hkv] fp32; all four change in place."""
+    Hkv, D = k_new.shape[-2:]
+    dev = k_cache.device
+    num_pages, page_size = _cache_shapes("treeflash_cache_append", k_cache, v_cache, k_scale, v_scale, Hkv, D)
+    N = slot.numel()
+    _shapes("treeflash_cache_append", v_new=(v_new, k_new.shape), slot=(slot, (N,)), source=(source, (N,)))
+    dt = _dtype_code(k_new)
+    kp, ld = _rows_ptr(k_new, "k_new", 2, k_new.dtype, dev)
+    vp, ldv = _rows_ptr(v_new, "v_new", 2, k_new.dtype, dev)
+    if ld != ldv:
+        raise ValueError("treeflash_cache_append: k_new and v_new must have the same strides")
+    if N == 0 or k_new.numel() == 0:
+        return
+    _launch("treeflash_cache_append", dev, kp, vp, ld, k_new.numel() // (Hkv * D), _ptr(slot, "slot", torch.int32, dev),
+            _ptr(source, "source", torch.int32, dev), N, Hkv, D, page_size, num_pages, dt,
+            _ptr(k_cache, "k_cache", E4M3, dev), _ptr(v_cache, "v_cache", E4M3, dev),
+            _ptr(k_scale, "k_scale", torch.float32, dev), _ptr(v_scale, "v_scale", torch.float32, dev))
+
+
+def treeflash_tree_attention_workspace_bytes(b, n, Hq, Hkv, D, page_size, max_pages, dtype) -> int:
+    code = dtype if isinstance(dtype, int) else (TF_BF16 if dtype == torch.bfloat16 else TF_F32)
+    return int(lib().treeflash_tree_attention_workspace_bytes(b, n, Hq, Hkv, D, page_size, max_pages, code))
+
+
+def treeflash_tree_attention(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, mask: Optional[torch.Tensor],
+                             context_len: torch.Tensor, block_table: torch.Tensor, k_cache: torch.Tensor,
+                             v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, scale: float,
+                             new_len: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                             out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+    """Attention of q [b, n, Hq, D] over each sequence's cached tokens and over the new positions themselves,
+    k_new and v_new [b, n, Hkv, D], as mask [b, n, n] (uint8, treeflash_tree_attention_inputs) admits them
+    (None: positions up to their own).  q, k_new and v_new may be views of one projection's rows.  Returns
+    out [b, n, Hq, D] and lse [b, n, Hq]; positions from new_len[s] on stay as they were."""
+    b, n, Hq, D = q.shape
+    Hkv = k_new.shape[2]
+    dev = q.device
+    max_pages = block_table.shape[1]
+    func = "treeflash_tree_attention"
+    num_pages, page_size = _cache_shapes(func, k_cache, v_cache, k_scale, v_scale, Hkv, D)
+    _shapes(func, k_new=(k_new, (b, n, Hkv, D)), v_new=(v_new, (b, n, Hkv, D)), mask=(mask, (b, n, n)),
+            context_len=(context_len, (b,)), block_table=(block_table, (b, max_pages)), new_len=(new_len, (b,)),
+            out=(out, (b, n, Hq, D)), lse=(lse, (b, n, Hq)))
+    dt = _dtype_code(q)
+    qp, ldq = _rows_ptr(q, "q", 2, q.dtype, dev)
+    kp, ld = _rows_ptr(k_new, "k_new", 2, q.dtype, dev)
+    vp, ldv = _rows_ptr(v_new, "v_new", 2, q.dtype, dev)
+    if ld != ldv:
+        raise ValueError(f"{func}: k_new and v_new must have the same strides")
+    if out is None:
+        out = torch.empty((b, n, Hq, D), dtype=q.dtype, device=dev)
+    if lse is None:
+        lse = torch.empty((b, n, Hq), dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = alloc_workspace(
+            treeflash_tree_attention_workspace_bytes(b, n, Hq, Hkv, D, page_size, max_pages, dt), dev)
+    i32, f32 = torch.int32, torch.float32
+    _launch(func, dev, qp, ldq, kp, vp, ld, _ptr(mask, "mask", torch.uint8, dev), _ptr(new_len, "new_len", i32, dev),
+            _ptr(context_len, "context_len", i32, dev), _ptr(block_table, "block_table", i32, dev),
+            _ptr(k_cache, "k_cache", E4M3, dev), _ptr(v_cache, "v_cache", E4M3, dev), _ptr(k_scale, "k_scale", f32, dev),
+            _ptr(v_scale, "v_scale", f32, dev), b, n, Hq, Hkv, D, page_size, max_pages, num_pages, float(scale), dt,
+            _ptr(out, "out", q.dtype, dev), _ptr(lse, "lse", f32, dev), _ptr(workspace, "workspace", device=dev),
+            workspace.numel() * workspace.element_size())
+    return out, lse
 
 
 class MarginalDrafter:

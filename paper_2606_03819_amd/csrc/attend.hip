@@ -1,0 +1,234 @@
+// Attention of a tree's positions over the paged 8-bit cache and the tree.
+//
+// A row is one query head at one position.  With t running over the cached
+// tokens and the new positions that the mask admits,
+//   out = sum_t w_t v_t / sum_t w_t,   w_t = 2^(x_t - m),
+//   x_t = log2(e) * scale * q.k_t,
+// in one pass: m is the running maximum, and sums made under an older one are
+// scaled by 2^(old - new).  Ranges of a long context are worked on side by
+// side and joined by merge_kernel in the same way.
+#include "attend.hpp"
+
+namespace tf {
+
+template <class T>
+__device__ __forceinline__ float load1(const T* p);
+template <>
+__device__ __forceinline__ float load1<uint16_t>(const uint16_t* p) { return bf16_bits_to_f32(*p); }
+template <>
+__device__ __forceinline__ float load1<float>(const float* p) { return *p; }
+
+// Workgroup (position, up to kGroupRows heads of one key head, range): its
+// waves take 64 tokens in turn.  For the products q.k a lane is a token, for
+// the sums over values a dimension, so both read 16 contiguous codes a lane
+// and the weights change places through LDS.
+template <class T, int D>
+__global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs a) {
+    constexpr int kDims = D / kWave;
+    __shared__ float qs[kGroupRows][D];
+    __shared__ float ps[kAttendWaves][kGroupRows][kWave];
+    __shared__ float sm[kAttendWaves][kGroupRows], sl[kAttendWaves][kGroupRows];
+    __shared__ float so[kAttendWaves][kGroupRows][D];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int s = blockIdx.x / a.n, i = blockIdx.x % a.n;
+    const int nl = new_of(a, s);
+    const int ctx = context_of(a, s);
+    const Split sp = split_context(ctx, a.splits);
+    if (i >= nl || (int)blockIdx.z >= sp.count) return;   // uniform
+    const int group = a.Hq / a.Hkv, blocks = (group + kGroupRows - 1) / kGroupRows;
+    const int hk = blockIdx.y / blocks, g0 = (blockIdx.y % blocks) * kGroupRows;
+    const int ng = min(kGroupRows, group - g0);
+    const int head0 = hk * group + g0;
+    const T* q = static_cast<const T*>(a.q) + (size_t)blockIdx.x * a.ld_q + (size_t)head0 * D;
+    for (int e = tid; e < kGroupRows * D; e += kAttendThreads)
+        qs[e / D][e % D] = e / D < ng ? load1(q + e) * (a.scale * kLog2e) : 0.f;
+    __syncthreads();
+
+    float m[kGroupRows], l[kGroupRows], o[kGroupRows][kDims];
+    for (int g = 0; g < kGroupRows; ++g) {
+        m[g] = neg_inf();
+        l[g] = 0.f;
+        for (int c = 0; c < kDims; ++c) o[g][c] = 0.f;
+    }
+    // the lane's products x become weights: LDS gets them, m, l and o follow
+    auto weigh = [&](const float* x) {
+        for (int g = 0; g < kGroupRows; ++g) {
+            const float mn = fmaxf(m[g], wave_max(x[g]));
+            const float back = mn == neg_inf() ? 1.f : exp2f(m[g] - mn);   // 0 from an empty start
+            const float p = mn == neg_inf() ? 0.f : exp2f(x[g] - mn);
+            m[g] = mn;
+            l[g] = l[g] * back + p;
+            for (int c = 0; c < kDims; ++c) o[g][c] *= back;
+            ps[wave][g][lane] = p;
+        }
+    };
+
+    const int32_t* table = a.block_table + (size_t)s * a.max_pages;
+    const int lo = blockIdx.z * sp.chunk, hi = min(ctx, lo + sp.chunk);
+    for (int t0 = lo + wave * kWave; t0 < hi; t0 += kAttendThreads) {
+        const int t = t0 + lane;
+        int id = t < hi ? table[t / a.page] : -1;
+        if (id >= a.num_pages) id = -1;
+        float x[kGroupRows] = {};
+        if (id >= 0) {
+            const size_t head = (size_t)id * a.Hkv + hk;
+            const u32x4* k = reinterpret_cast<const u32x4*>(a.k_cache + head * a.page * D + (size_t)(t & (a.page - 1)) * D);
+            for (int c = 0; c < D / 16; ++c) {
+                const u32x4 w = k[c];
+                for (int e = 0; e < 4; ++e) {
+                    const f32pair u = e4m3_pair<false>(w[e]), v = e4m3_pair<true>(w[e]);
+                    for (int g = 0; g < kGroupRows; ++g) {
+                        const float* qq = &qs[g][c * 16 + e * 4];
+                        x[g] += qq[0] * u[0] + qq[1] * u[1] + qq[2] * v[0] + qq[3] * v[1];
+                    }
+                }
+            }
+            const float ks = a.k_scale[head];
+            for (int g = 0; g < kGroupRows; ++g) x[g] *= ks;
+        } else {
+            for (int g = 0; g < kGroupRows; ++g) x[g] = neg_inf();
+        }
+        weigh(x);
+        for (int part = 0; part < kWave / 16; ++part) {   // 16 tokens lie in one page
+            const int first = t0 + part * 16;
+            if (first >= hi) break;
+            const int page = __shfl(id, part * 16);
+            if (page < 0) continue;
+            const size_t head = (size_t)page * a.Hkv + hk;
+            const float vs = a.v_scale[head];
+            for (int c = 0; c < kDims; ++c) {
+                const u32x4 w = *reinterpret_cast<const u32x4*>(
+                    a.v_cache + head * a.page * D + (size_t)(c * kWave + lane) * a.page + (first & (a.page - 1)));
+                for (int e = 0; e < 4; ++e) {
+                    const f32pair u = e4m3_pair<false>(w[e]), v = e4m3_pair<true>(w[e]);
+                    const float y[4] = {u[0], u[1], v[0], v[1]};
+                    for (int j = 0; j < 4; ++j) {
+                        const int tt = e * 4 + j;
+                        const float val = first + tt < hi ? y[j] * vs : 0.f;   // what lies behind may be NaN
+                        for (int g = 0; g < kGroupRows; ++g) o[g][c] += ps[wave][g][part * 16 + tt] * val;
+                    }
+                }
+            }
+        }
+    }
+    if ((int)blockIdx.z == sp.count - 1) {   // the new positions go with the last range
+        const uint8_t* mask = a.mask != nullptr ? a.mask + (size_t)blockIdx.x * a.n : nullptr;
+        for (int j0 = wave * kWave; j0 < nl; j0 += kAttendThreads) {
+            const int j = j0 + lane;
+            const bool sees = j < nl && (mask != nullptr ? mask[j] != 0 : j <= i);
+            unsigned long long todo = __ballot(sees);
+            if (todo == 0) continue;
+            float x[kGroupRows];
+            for (int g = 0; g < kGroupRows; ++g) x[g] = sees ? 0.f : neg_inf();
+            if (sees) {
+                const T* k = static_cast<const T*>(a.k_new) + ((size_t)s * a.n + j) * a.ld_new + (size_t)hk * D;
+                for (int d = 0; d < D; ++d) {
+                    const float kv = load1(k + d);
+                    for (int g = 0; g < kGroupRows; ++g) x[g] += qs[g][d] * kv;
+                }
+            }
+            weigh(x);
+            while (todo != 0) {
+                const int jj = __builtin_ctzll(todo);
+                todo &= todo - 1;
+                const T* v = static_cast<const T*>(a.v_new) + ((size_t)s * a.n + j0 + jj) * a.ld_new + (size_t)hk * D;
+                for (int c = 0; c < kDims; ++c) {
+                    const float val = load1(v + c * kWave + lane);
+                    for (int g = 0; g < kGroupRows; ++g) o[g][c] += ps[wave][g][jj] * val;
+                }
+            }
+        }
+    }
+    for (int g = 0; g < kGroupRows; ++g) {
+        const float sum = wave_sum(l[g]);
+        if (lane == 0) sm[wave][g] = m[g], sl[wave][g] = sum;
+        for (int c = 0; c < kDims; ++c) so[wave][g][c * kWave + lane] = o[g][c];
+    }
+    __syncthreads();
+    for (int e = tid; e < ng * D; e += kAttendThreads) {
+        const int g = e / D, d = e % D;
+        float mt = neg_inf();
+        for (int w = 0; w < kAttendWaves; ++w) mt = fmaxf(mt, sm[w][g]);
+        float lt = 0.f, ot = 0.f;
+        for (int w = 0; w < kAttendWaves; ++w) {
+            const float f = sl[w][g] > 0.f ? exp2f(sm[w][g] - mt) : 0.f;
+            lt += sl[w][g] * f;
+            ot += so[w][g][d] * f;
+        }
+        const size_t row = (size_t)blockIdx.x * a.Hq + head0 + g;
+        if (sp.count == 1) {
+            store_out(a.out, row * D + d, lt > 0.f ? ot / lt : 0.f, sizeof(T) == 2);
+            if (d == 0 && a.lse != nullptr) a.lse[row] = lse_of(mt, lt);
+        } else {
+            float* p = part_of(a, row, blockIdx.z, D);
+            p[d] = ot;
+            if (d == 0) p[D] = mt, p[D + 1] = lt;
+        }
+    }
+}
+
+// One wave a row: the ranges of a split context joined.
+template <class T, int D>
+__global__ __launch_bounds__(kAttendThreads) void merge_kernel(AttendArgs a) {
+    const int lane = threadIdx.x & 63;
+    const size_t row = (size_t)blockIdx.x * kAttendWaves + (threadIdx.x >> 6);
+    if (row >= (size_t)a.b * a.n * a.Hq) return;
+    const int s = (int)(row / ((size_t)a.n * a.Hq)), i = (int)(row / a.Hq % a.n);
+    const int count = split_context(context_of(a, s), a.splits).count;
+    if (count == 1 || i >= new_of(a, s)) return;
+    float m = neg_inf(), l = 0.f, o[D / kWave] = {};
+    for (int sp = 0; sp < count; ++sp) {
+        const float* p = part_of(a, row, sp, D);
+        const float mp = p[D], lp = p[D + 1];
+        if (!(lp > 0.f)) continue;
+        const float mn = fmaxf(m, mp), fa = exp2f(m - mn), fb = exp2f(mp - mn);
+        m = mn;
+        l = l * fa + lp * fb;
+        for (int c = 0; c < D / kWave; ++c) o[c] = o[c] * fa + p[c * kWave + lane] * fb;
+    }
+    for (int c = 0; c < D / kWave; ++c) store_out(a.out, row * D + c * kWave + lane, l > 0.f ? o[c] / l : 0.f, sizeof(T) == 2);
+    if (lane == 0 && a.lse != nullptr) a.lse[row] = lse_of(m, l);
+}
+
+namespace {
+
+// Ranges a context is split into at most: enough for about 1024 workgroups.
+int most_splits(long long groups, int max_pages, int page) {
+    const long long longest = ((long long)max_pages * page + kSplitLeast - 1) / kSplitLeast;
+    long long want = (1024 + groups - 1) / groups;
+    want = want < longest ? want : longest;
+    return (int)(want < 1 ? 1 : want > 64 ? 64 : want);
+}
+
+long long row_groups(int b, int n, int Hq, int Hkv) {
+    const int blocks = (Hq / Hkv + kGroupRows - 1) / kGroupRows;
+    return (long long)b * n * Hkv * blocks;
+}
+
+template <class T, int D>
+hipError_t launch_rows(const AttendArgs& a, hipStream_t stream) {
+    const int blocks = (a.Hq / a.Hkv + kGroupRows - 1) / kGroupRows;
+    hipLaunchKernelGGL((attend_rows_kernel<T, D>), dim3(a.b * a.n, a.Hkv * blocks, a.splits), dim3(kAttendThreads), 0,
+                       stream, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    const long long rows = (long long)a.b * a.n * a.Hq;
+    hipLaunchKernelGGL((merge_kernel<T, D>), dim3((unsigned)((rows + kAttendWaves - 1) / kAttendWaves)),
+                       dim3(kAttendThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attend_part_bytes(int b, int n, int Hq, int Hkv, int D, int page, int max_pages, bool bf16) {
+    const int splits = most_splits(row_groups(b, n, Hq, Hkv), max_pages, page);
+    return splits == 1 ? 0 : (size_t)splits * b * n * Hq * (D + 2) * 4;
+}
+
+hipError_t launch_tree_attention(AttendArgs a, int D, bool bf16, hipStream_t stream) {
+    a.splits = most_splits(row_groups(a.b, a.n, a.Hq, a.Hkv), a.max_pages, a.page);
+    if (bf16) return D == 128 ? launch_rows<uint16_t, 128>(a, stream) : launch_rows<uint16_t, 64>(a, stream);
+    return D == 128 ? launch_rows<float, 128>(a, stream) : launch_rows<float, 64>(a, stream);
+}
+
+}  // namespace tf

@@ -1,0 +1,51 @@
+// Attention over the paged 8-bit cache: what its kernels share.
+#pragma once
+
+#include "common.hpp"
+#include "e4m3.hpp"
+#include "launch.hpp"
+
+namespace tf {
+
+constexpr int kAttendThreads = 256;
+constexpr int kAttendWaves = kAttendThreads / kWave;
+constexpr int kGroupRows = 4;   // query heads of one position that a workgroup of the row kernel serves
+
+// The ranges that a context of `ctx` tokens is split into: at most `most`, of
+// kSplitLeast tokens at least, each a multiple of 64 but the last.
+constexpr int kSplitLeast = 256;
+struct Split {
+    int chunk, count;
+};
+__host__ __device__ inline Split split_context(int ctx, int most) {
+    int e = (ctx + kSplitLeast - 1) / kSplitLeast;
+    e = e < most ? e : most;
+    e = e > 1 ? e : 1;
+    int chunk = ((ctx + e - 1) / e + 63) & ~63;
+    chunk = chunk > 64 ? chunk : 64;
+    const int count = (ctx + chunk - 1) / chunk;
+    return {chunk, count > 1 ? count : 1};
+}
+
+__device__ __forceinline__ int context_of(const AttendArgs& a, int s) {
+    return min(max(a.context_len[s], 0), a.max_pages * a.page);
+}
+__device__ __forceinline__ int new_of(const AttendArgs& a, int s) {
+    return a.new_len == nullptr ? a.n : min(max(a.new_len[s], 0), a.n);
+}
+
+// Partials of split contexts: for row r = (s*n + i)*Hq + head and range sp,
+// D sums, then the running maximum (base 2) and the sum of weights.
+__device__ __forceinline__ float* part_of(const AttendArgs& a, size_t row, int sp, int D) {
+    return a.part + ((size_t)sp * a.b * a.n * a.Hq + row) * (D + 2);
+}
+
+__device__ __forceinline__ void store_out(void* out, size_t at, float v, bool bf16) {
+    if (bf16) static_cast<uint16_t*>(out)[at] = (uint16_t)f32_to_bf16_bits(v);
+    else static_cast<float*>(out)[at] = v;
+}
+
+// A finished row: sums over weights (none: zeros and -inf).
+__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + __log2f(l)) * kLn2 : neg_inf(); }
+
+}  // namespace tf

@@ -1,0 +1,342 @@
+// The paged 8-bit cache: pages and slots from lengths (cache_plan_kernel,
+// cache_fill_kernel, cache_release_kernel), keys and values into it
+// (cache_append_kernel).
+#include "common.hpp"
+#include "e4m3.hpp"
+#include "launch.hpp"
+
+namespace tf {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kFillThreads = 256;
+constexpr int kFillPer = 4;            // tokens a thread of the fill places
+// Tokens up to which the planning workgroup fills the lists itself, which
+// saves the second launch.
+constexpr int kFillAlone = 1 << 14;
+
+__device__ __forceinline__ int pages_of(int len, int page) { return (len + page - 1) / page; }
+
+// Inclusive sum over the workgroup's threads (all call); `tmp` holds one
+// value a wave and is free again on return.
+__device__ __forceinline__ long long block_scan(long long v, long long* tmp) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    for (int o = 1; o < 64; o <<= 1) {
+        const long long up = __shfl_up(v, o);
+        if (lane >= o) v += up;
+    }
+    if (lane == 63) tmp[wave] = v;
+    __syncthreads();
+    long long before = 0;
+    for (int w = 0; w < waves; ++w) before += w < wave ? tmp[w] : 0;
+    __syncthreads();
+    return v + before;
+}
+
+// Places tokens [i0, i1) of the lists.  `start` and `page_start` are whole
+// and new_len, new_free_count written: the old length of a sequence is its
+// new one less its tokens, and its pages sit below the old top of the stack.
+__device__ void fill_slots(const SlotsArgs& a, int i0, int i1, int step) {
+    const int total = a.start[a.b];
+    const int top = a.new_free_count[0] + a.page_start[a.b];   // pages on the stack before the call
+    for (int i = i0; i < i1; i += step) {
+        int sl = -1, ps = -1, src = -1;
+        if (i < total) {
+            int lo = 0, hi = a.b;   // start[lo] <= i < start[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.start[mid] <= i) lo = mid;
+                else hi = mid;
+            }
+            const int s = lo, j = i - a.start[s];
+            const int ctx = a.new_len[s] - (a.start[s + 1] - a.start[s]);
+            ps = ctx + j;
+            const int col = ps / a.page, off = ps - col * a.page;
+            const int had = pages_of(ctx, a.page);
+            const size_t at = (size_t)s * a.max_pages + col;
+            int id;
+            if (col < had) {
+                id = a.block_table[at];
+            } else {
+                id = a.free_pages[top - 1 - (a.page_start[s] + col - had)];
+                if (off == 0) a.block_table[at] = id;   // a new page's first token is a new token
+            }
+            const long long slot = (long long)id * a.page + off;
+            sl = id >= 0 && slot <= 0x7fffffffll ? (int)slot : -1;
+            const long long row = a.n == 0 ? i
+                                           : (long long)s * a.n +
+                                                 (a.accepted == nullptr ? j : (j == 0 ? 0 : 1 + a.accepted[(size_t)s * a.gamma + j - 1]));
+            src = (int)row;
+        }
+        a.slot[i] = sl;
+        if (a.position != nullptr) a.position[i] = ps;
+        if (a.source != nullptr) a.source[i] = src;
+    }
+}
+
+// One workgroup: sums of tokens and pages over the sequences, whether all of
+// them fit, then lengths and list offsets; `alone`: the lists as well.  What
+// bounds it is the chain of loads and two scans, about a launch.  All reads of
+// lengths and count end before the first write (new_len and new_free_count
+// may be the same arrays).
+__global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(SlotsArgs a, int alone) {
+    __shared__ long long tmp[kPlanThreads / 64];
+    __shared__ long long carry_tok, carry_page;
+    __shared__ int bad;
+    const int tid = threadIdx.x;
+    const int extra = a.accepted != nullptr ? 1 : 0;
+    if (tid == 0) bad = 0, carry_tok = 0, carry_page = 0;
+    __syncthreads();
+    const int left = a.free_count[0];
+    long long tok = 0, pg = 0;
+    int wrong = left < 0 || left > a.max_free ? 1 : 0, wide = 0;
+    for (int s = tid; s < a.b; s += kPlanThreads) {
+        const int ctx = a.context_len[s], add = a.add_len[s];
+        if (ctx < 0 || add < 0 || (extra && add > a.gamma) || (a.n > 0 && (long long)add + extra > a.n)) {
+            wrong = 1;
+            continue;
+        }
+        const long long after = (long long)ctx + add + extra;
+        tok += add + extra;
+        if (after > (long long)a.max_pages * a.page) {
+            wide = 1;
+            continue;
+        }
+        pg += pages_of((int)after, a.page) - pages_of(ctx, a.page);
+    }
+    if (wrong) atomicOr(&bad, 1);
+    if (wide) atomicOr(&bad, 2);
+    tok = block_scan(tok, tmp);
+    pg = block_scan(pg, tmp);
+    if (tid == kPlanThreads - 1) carry_tok = tok, carry_page = pg;
+    __syncthreads();
+    const long long all_tok = carry_tok, all_page = carry_page;
+    const int status = (bad & 1) ? 1 : all_tok > a.max_tokens ? 2 : (bad & 2) ? 3 : all_page > left ? 4 : 0;
+    __syncthreads();
+    if (tid == 0) {
+        carry_tok = carry_page = 0;
+        a.status[0] = status;
+        a.start[0] = 0;
+        a.page_start[0] = 0;
+        a.new_free_count[0] = status == 0 ? left - (int)all_page : left;
+    }
+    for (int s0 = 0; s0 < a.b; s0 += kPlanThreads) {
+        const int s = s0 + tid;
+        int ctx = 0, add = 0, need = 0;
+        if (s < a.b) {
+            ctx = a.context_len[s];
+            if (status == 0) {
+                add = a.add_len[s] + extra;
+                need = pages_of(ctx + add, a.page) - pages_of(ctx, a.page);
+            }
+        }
+        const long long t = block_scan(add, tmp), p = block_scan(need, tmp);
+        const long long bt = carry_tok, bp = carry_page;   // written before the scans' barriers
+        if (s < a.b) {
+            a.start[s + 1] = (int)(bt + t);
+            a.page_start[s + 1] = (int)(bp + p);
+            a.new_len[s] = ctx + add;
+        }
+        __syncthreads();
+        if (tid == kPlanThreads - 1) carry_tok = bt + t, carry_page = bp + p;
+        __syncthreads();
+    }
+    if (alone) {
+        __threadfence_block();
+        __syncthreads();
+        fill_slots(a, tid, a.max_tokens, kPlanThreads);
+    }
+}
+
+__global__ __launch_bounds__(kFillThreads) void cache_fill_kernel(SlotsArgs a) {
+    const int i0 = blockIdx.x * (kFillThreads * kFillPer);
+    fill_slots(a, i0 + threadIdx.x, min(i0 + kFillThreads * kFillPer, a.max_tokens), kFillThreads);
+}
+
+// One workgroup: the finished sequences' pages go onto the stack in order.
+__global__ __launch_bounds__(kPlanThreads) void cache_release_kernel(ReleaseArgs a) {
+    __shared__ long long tmp[kPlanThreads / 64];
+    __shared__ long long carry;
+    const int tid = threadIdx.x;
+    const int count = min(max(a.free_count[0], 0), a.max_free);
+    if (tid == 0) carry = count;
+    __syncthreads();
+    for (int s0 = 0; s0 < a.b; s0 += kPlanThreads) {
+        const int s = s0 + tid;
+        int len = 0, give = 0;
+        bool done = false;
+        if (s < a.b) {
+            len = a.context_len[s];
+            done = a.done[s] != 0;
+            if (done && len > 0) give = (int)min((long long)len + a.page - 1, (long long)a.max_pages * a.page) / a.page;
+        }
+        const long long t = block_scan(give, tmp);
+        const long long at = carry + t - give;
+        for (int p = 0; p < give; ++p)
+            if (at + p < a.max_free) a.free_pages[at + p] = a.block_table[(size_t)s * a.max_pages + p];
+        if (s < a.b) a.new_len[s] = done ? 0 : len;
+        __syncthreads();
+        if (tid == kPlanThreads - 1) carry += t;
+        __syncthreads();
+    }
+    if (tid == 0) a.new_free_count[0] = (int)min(carry, (long long)a.max_free);
+}
+
+// ------------------------------------------------------------------ append
+
+constexpr int kAppendThreads = 256;
+
+template <class T>
+__device__ __forceinline__ void load8(const T* p, float* x);
+template <>
+__device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float* x) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = bf16_bits_to_f32(w[i] & 0xffffu);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, float* x) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+}
+
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = fabsf(x);
+    return a < __builtin_inff() ? a : 0.f;   // neither infinities nor NaN enter the scale
+}
+
+// Workgroup (`per` tokens of the list, head): for each run that begins among
+// its tokens, the run's largest values, the scale, what the page held rounded
+// again where the scale rose, the new codes.  The page's first token of the
+// list leads its run, so every page and head has one writer and no atomics.
+// The rows are read twice, the second time from the cache.  Values are turned
+// in LDS, so that the [D, page] side stores dwords of four tokens.
+template <class T, int D>
+__global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs a, int per) {
+    constexpr int kChunks = D / 8;                          // threads across a row
+    constexpr int kRowsPass = kAppendThreads / kChunks;
+    constexpr int kPitch = 128 + 4;                         // tokens of a page and a dword, against bank conflicts
+    __shared__ __align__(16) uint8_t turned[D * kPitch];
+    __shared__ float s_max[2][kAppendThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int h = blockIdx.y;
+    const int end = (int)min((long long)a.N, (long long)(blockIdx.x + 1) * per);
+    const long long limit = (long long)a.num_pages * a.page;
+    const int c8 = (tid % kChunks) * 8, r0 = tid / kChunks;
+    const T* kn = static_cast<const T*>(a.k_new) + (size_t)h * D + c8;
+    const T* vn = static_cast<const T*>(a.v_new) + (size_t)h * D + c8;
+    for (int i = (int)blockIdx.x * per; i < end; ++i) {     // uniform over the workgroup
+        const int sl = a.slot[i];
+        if (sl < 0 || sl >= limit) continue;
+        const int off = sl & (a.page - 1), id = sl / a.page;
+        if (off != 0 && i > 0 && a.slot[i - 1] == sl - 1) continue;
+        const int most = min(a.page - off, a.N - i);
+        const unsigned long long b0 = __ballot(lane < most && a.slot[i + min(lane, most - 1)] == sl + lane);
+        const unsigned long long b1 = __ballot(lane + 64 < most && a.slot[i + min(lane + 64, most - 1)] == sl + lane + 64);
+        const int run = ~b0 != 0 ? __builtin_ctzll(~b0) : (~b1 != 0 ? 64 + __builtin_ctzll(~b1) : 128);
+
+        float mk = 0.f, mv = 0.f;
+        for (int j = r0; j < run; j += kRowsPass) {
+            const int row = a.source != nullptr ? a.source[i + j] : i + j;
+            if (row < 0 || row >= a.rows) continue;
+            float x[8];
+            load8(kn + (size_t)row * a.ld_new, x);
+            for (int e = 0; e < 8; ++e) mk = fmaxf(mk, finite_abs(x[e]));
+            load8(vn + (size_t)row * a.ld_new, x);
+            for (int e = 0; e < 8; ++e) mv = fmaxf(mv, finite_abs(x[e]));
+        }
+        mk = wave_max(mk);
+        mv = wave_max(mv);
+        if (lane == 0) s_max[0][wave] = mk, s_max[1][wave] = mv;
+        __syncthreads();
+        for (int w = 0; w < kAppendThreads / 64; ++w) {
+            mk = fmaxf(mk, s_max[0][w]);
+            mv = fmaxf(mv, s_max[1][w]);
+        }
+        const size_t head = (size_t)id * a.Hkv + h;
+        float sk = pow2_scale(mk), sv = pow2_scale(mv);
+        const float ok = off > 0 ? a.k_scale[head] : 0.f, ov = off > 0 ? a.v_scale[head] : 0.f;
+        sk = fmaxf(sk, ok);
+        sv = fmaxf(sv, ov);
+        uint8_t* kc = static_cast<uint8_t*>(a.k_cache) + head * a.page * D;
+        uint8_t* vc = static_cast<uint8_t*>(a.v_cache) + head * a.page * D;
+        if (off > 0 && sk != ok) {
+            uint32_t* p = reinterpret_cast<uint32_t*>(kc);
+            for (int e = tid; e < off * (D / 4); e += kAppendThreads) p[e] = e4m3_rescale(p[e], ok / sk);
+        }
+        if (off > 0 && sv != ov) {
+            const int quads = (off + 3) / 4;
+            for (int e = tid; e < D * quads; e += kAppendThreads) {
+                const int d = e / quads, t = (e - d * quads) * 4;
+                uint8_t* p = vc + (size_t)d * a.page + t;
+                const uint32_t w = e4m3_rescale(*reinterpret_cast<const uint32_t*>(p), ov / sv);
+                if (t + 4 <= off) *reinterpret_cast<uint32_t*>(p) = w;
+                else   // the dword that the run goes on in
+                    for (int q = 0; t + q < off; ++q) p[q] = (uint8_t)(w >> (8 * q));
+            }
+        }
+        const float ik = 1.f / sk, iv = 1.f / sv;   // powers of two: exact
+        for (int j = r0; j < run; j += kRowsPass) {
+            const int row = a.source != nullptr ? a.source[i + j] : i + j;
+            const bool real = row >= 0 && row < a.rows;
+            float x[8] = {}, y[8] = {};
+            if (real) {
+                load8(kn + (size_t)row * a.ld_new, x);
+                load8(vn + (size_t)row * a.ld_new, y);
+            }
+            uint32_t* kd = reinterpret_cast<uint32_t*>(kc + (size_t)(off + j) * D + c8);
+            kd[0] = e4m3_quad(x[0] * ik, x[1] * ik, x[2] * ik, x[3] * ik);
+            kd[1] = e4m3_quad(x[4] * ik, x[5] * ik, x[6] * ik, x[7] * ik);
+            const uint32_t lo = e4m3_quad(y[0] * iv, y[1] * iv, y[2] * iv, y[3] * iv);
+            const uint32_t hi = e4m3_quad(y[4] * iv, y[5] * iv, y[6] * iv, y[7] * iv);
+            for (int e = 0; e < 8; ++e) turned[(c8 + e) * kPitch + off + j] = (uint8_t)((e < 4 ? lo : hi) >> (8 * (e & 3)));
+        }
+        __syncthreads();
+        const int q0 = off / 4, quads = (off + run + 3) / 4 - q0;
+        for (int e = tid; e < D * quads; e += kAppendThreads) {
+            const int d = e / quads, t = (q0 + e - d * quads) * 4;
+            const uint8_t* from = turned + d * kPitch + t;
+            uint8_t* p = vc + (size_t)d * a.page + t;
+            if (t >= off && t + 4 <= off + run) *reinterpret_cast<uint32_t*>(p) = *reinterpret_cast<const uint32_t*>(from);
+            else
+                for (int q = 0; q < 4; ++q)
+                    if (t + q >= off && t + q < off + run) p[q] = from[q];
+        }
+        if (tid == 0) a.k_scale[head] = sk, a.v_scale[head] = sv;
+        __syncthreads();   // `turned` and s_max are free again
+    }
+}
+
+hipError_t launch_cache_slots(const SlotsArgs& a, hipStream_t stream) {
+    const int alone = a.max_tokens <= kFillAlone ? 1 : 0;
+    hipLaunchKernelGGL(cache_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, alone);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || alone) return e;
+    const int per = kFillThreads * kFillPer;
+    hipLaunchKernelGGL(cache_fill_kernel, dim3((a.max_tokens - 1) / per + 1), dim3(kFillThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_release(const ReleaseArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL(cache_release_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_append(const AppendArgs& a, int D, bool bf16, hipStream_t stream) {
+    // about 8192 workgroups: single tokens get one each, long lists share one among up to a page
+    int per = 1;
+    while (per < 64 && (long long)a.N * a.Hkv > 8192ll * per) per *= 2;
+    const dim3 grid((unsigned)((a.N - 1) / per + 1), (unsigned)a.Hkv);
+    if (bf16 && D == 128)
+        hipLaunchKernelGGL((cache_append_kernel<uint16_t, 128>), grid, dim3(kAppendThreads), 0, stream, a, per);
+    else if (bf16)
+        hipLaunchKernelGGL((cache_append_kernel<uint16_t, 64>), grid, dim3(kAppendThreads), 0, stream, a, per);
+    else if (D == 128)
+        hipLaunchKernelGGL((cache_append_kernel<float, 128>), grid, dim3(kAppendThreads), 0, stream, a, per);
+    else
+        hipLaunchKernelGGL((cache_append_kernel<float, 64>), grid, dim3(kAppendThreads), 0, stream, a, per);
+    return hipGetLastError();
+}
+
+}  // namespace tf

@@ -58,4 +58,68 @@ hipError_t launch_tree_inputs(const int32_t* root_token, const int32_t* node_tok
 hipError_t launch_accept(const int32_t* node_token, const int32_t* node_parent, const int32_t* target, int b, int B,
                          int max_depth, int32_t* accepted, int32_t* accept_len, int32_t* bonus, hipStream_t stream);
 
+// Pages and slots of the tokens that sequences gain (treeflash_cache_slots).
+struct SlotsArgs {
+    const int32_t *context_len, *add_len, *accepted, *free_pages, *free_count;
+    int b, gamma, n, page, max_pages, max_free, max_tokens;
+    int32_t *block_table, *new_len, *new_free_count, *start, *page_start, *slot, *position, *source, *status;
+};
+hipError_t launch_cache_slots(const SlotsArgs& a, hipStream_t stream);
+
+// Pages of finished sequences back onto the stack (treeflash_cache_release).
+struct ReleaseArgs {
+    const uint8_t* done;
+    const int32_t *context_len, *block_table, *free_count;
+    int b, page, max_pages, max_free;
+    int32_t *free_pages, *new_len, *new_free_count;
+};
+hipError_t launch_cache_release(const ReleaseArgs& a, hipStream_t stream);
+
+// Keys and values into the cache (treeflash_cache_append).
+struct AppendArgs {
+    const void *k_new, *v_new;
+    long long ld_new;
+    int rows;
+    const int32_t *slot, *source;
+    int N, Hkv, page, num_pages;
+    void *k_cache, *v_cache;
+    float *k_scale, *v_scale;
+};
+hipError_t launch_cache_append(const AppendArgs& a, int D, bool bf16, hipStream_t stream);
+
+// Attention over the cache and the new positions (treeflash_tree_attention).
+struct AttendArgs {
+    const void* q;
+    long long ld_q;
+    const void *k_new, *v_new;
+    long long ld_new;
+    const uint8_t* mask;
+    const int32_t *new_len, *context_len, *block_table;
+    const uint8_t *k_cache, *v_cache;
+    const float *k_scale, *v_scale;
+    int b, n, Hq, Hkv, page, max_pages, num_pages;
+    float scale;
+    void* out;
+    float* lse;
+    float* part;      // partials of split contexts
+    int splits;       // most ranges a context is split into
+};
+size_t attend_part_bytes(int b, int n, int Hq, int Hkv, int D, int page, int max_pages, bool bf16);
+hipError_t launch_tree_attention(AttendArgs a, int D, bool bf16, hipStream_t stream);
+
+// A token for each row of logits (treeflash_sample).
+struct SampleArgs {
+    const void* logits;
+    long long ld;
+    int n, rows, V;
+    const float* temperature;
+    const int32_t* top_k;
+    const float *top_p, *min_p, *uniform;
+    int32_t* token;
+    float* logprob;
+    unsigned char* ws;
+};
+size_t sample_ws_bytes(long long rows, int V);
+hipError_t launch_sample(const SampleArgs& a, bool bf16, hipStream_t stream);
+
 }  // namespace tf
