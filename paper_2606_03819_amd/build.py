@@ -19,7 +19,7 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_NAME = "libtreeflash.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
 SOURCES = ["lmhead.hip", "lmhead_tile.hip", "mlp.hip", "tile_product.hip", "tree.hip", "verify.hip", "sample.hip",
-           "cache.hip", "attend.hip", "api.cpp", "api_verify.cpp"]
+           "cache.hip", "attend.hip", "attend_tile.hip", "api.cpp", "api_verify.cpp"]
 ARCH = "gfx950"
 
 COMMON_FLAGS = [

@@ -11,18 +11,11 @@
 
 namespace tf {
 
-template <class T>
-__device__ __forceinline__ float load1(const T* p);
-template <>
-__device__ __forceinline__ float load1<uint16_t>(const uint16_t* p) { return bf16_bits_to_f32(*p); }
-template <>
-__device__ __forceinline__ float load1<float>(const float* p) { return *p; }
-
-// Workgroup (position, up to kGroupRows heads of one key head, range): its
+// fp32.  Workgroup (position, up to kGroupRows heads of one key head, range): its
 // waves take 64 tokens in turn.  For the products q.k a lane is a token, for
 // the sums over values a dimension, so both read 16 contiguous codes a lane
 // and the weights change places through LDS.
-template <class T, int D>
+template <int D>
 __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs a) {
     constexpr int kDims = D / kWave;
     __shared__ float qs[kGroupRows][D];
@@ -39,9 +32,9 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
     const int hk = blockIdx.y / blocks, g0 = (blockIdx.y % blocks) * kGroupRows;
     const int ng = min(kGroupRows, group - g0);
     const int head0 = hk * group + g0;
-    const T* q = static_cast<const T*>(a.q) + (size_t)blockIdx.x * a.ld_q + (size_t)head0 * D;
+    const float* q = static_cast<const float*>(a.q) + (size_t)blockIdx.x * a.ld_q + (size_t)head0 * D;
     for (int e = tid; e < kGroupRows * D; e += kAttendThreads)
-        qs[e / D][e % D] = e / D < ng ? load1(q + e) * (a.scale * kLog2e) : 0.f;
+        qs[e / D][e % D] = e / D < ng ? q[e] * (a.scale * kLog2e) : 0.f;
     __syncthreads();
 
     float m[kGroupRows], l[kGroupRows], o[kGroupRows][kDims];
@@ -55,7 +48,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
         for (int g = 0; g < kGroupRows; ++g) {
             const float mn = fmaxf(m[g], wave_max(x[g]));
             const float back = mn == neg_inf() ? 1.f : exp2f(m[g] - mn);   // 0 from an empty start
-            const float p = mn == neg_inf() ? 0.f : exp2f(x[g] - mn);
+            const float p = exp2f(x[g] - (mn == neg_inf() ? 0.f : mn));   // a NaN stays one
             m[g] = mn;
             l[g] = l[g] * back + p;
             for (int c = 0; c < kDims; ++c) o[g][c] *= back;
@@ -121,9 +114,9 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
             float x[kGroupRows];
             for (int g = 0; g < kGroupRows; ++g) x[g] = sees ? 0.f : neg_inf();
             if (sees) {
-                const T* k = static_cast<const T*>(a.k_new) + ((size_t)s * a.n + j) * a.ld_new + (size_t)hk * D;
+                const float* k = static_cast<const float*>(a.k_new) + ((size_t)s * a.n + j) * a.ld_new + (size_t)hk * D;
                 for (int d = 0; d < D; ++d) {
-                    const float kv = load1(k + d);
+                    const float kv = k[d];
                     for (int g = 0; g < kGroupRows; ++g) x[g] += qs[g][d] * kv;
                 }
             }
@@ -131,9 +124,9 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
             while (todo != 0) {
                 const int jj = __builtin_ctzll(todo);
                 todo &= todo - 1;
-                const T* v = static_cast<const T*>(a.v_new) + ((size_t)s * a.n + j0 + jj) * a.ld_new + (size_t)hk * D;
+                const float* v = static_cast<const float*>(a.v_new) + ((size_t)s * a.n + j0 + jj) * a.ld_new + (size_t)hk * D;
                 for (int c = 0; c < kDims; ++c) {
-                    const float val = load1(v + c * kWave + lane);
+                    const float val = v[c * kWave + lane];
                     for (int g = 0; g < kGroupRows; ++g) o[g][c] += ps[wave][g][jj] * val;
                 }
             }
@@ -151,18 +144,21 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
         for (int w = 0; w < kAttendWaves; ++w) mt = fmaxf(mt, sm[w][g]);
         float lt = 0.f, ot = 0.f;
         for (int w = 0; w < kAttendWaves; ++w) {
-            const float f = sl[w][g] > 0.f ? exp2f(sm[w][g] - mt) : 0.f;
+            const float f = sm[w][g] == neg_inf() ? 1.f : exp2f(sm[w][g] - mt);
             lt += sl[w][g] * f;
             ot += so[w][g][d] * f;
         }
         const size_t row = (size_t)blockIdx.x * a.Hq + head0 + g;
         if (sp.count == 1) {
-            store_out(a.out, row * D + d, lt > 0.f ? ot / lt : 0.f, sizeof(T) == 2);
+            static_cast<float*>(a.out)[row * D + d] = lt == 0.f ? 0.f : ot / lt;
             if (d == 0 && a.lse != nullptr) a.lse[row] = lse_of(mt, lt);
         } else {
-            float* p = part_of(a, row, blockIdx.z, D);
-            p[d] = ot;
-            if (d == 0) p[D] = mt, p[D + 1] = lt;
+            part_sums(a, row, blockIdx.z, D)[d] = ot;
+            if (d == 0) {
+                float* ml = part_stats(a, row, blockIdx.z, D);
+                ml[0] = mt;
+                ml[1] = lt;
+            }
         }
     }
 }
@@ -178,15 +174,15 @@ __global__ __launch_bounds__(kAttendThreads) void merge_kernel(AttendArgs a) {
     if (count == 1 || i >= new_of(a, s)) return;
     float m = neg_inf(), l = 0.f, o[D / kWave] = {};
     for (int sp = 0; sp < count; ++sp) {
-        const float* p = part_of(a, row, sp, D);
-        const float mp = p[D], lp = p[D + 1];
-        if (!(lp > 0.f)) continue;
+        const float* p = part_sums(a, row, sp, D);
+        const float mp = part_stats(a, row, sp, D)[0], lp = part_stats(a, row, sp, D)[1];
+        if (lp == 0.f) continue;
         const float mn = fmaxf(m, mp), fa = exp2f(m - mn), fb = exp2f(mp - mn);
         m = mn;
         l = l * fa + lp * fb;
         for (int c = 0; c < D / kWave; ++c) o[c] = o[c] * fa + p[c * kWave + lane] * fb;
     }
-    for (int c = 0; c < D / kWave; ++c) store_out(a.out, row * D + c * kWave + lane, l > 0.f ? o[c] / l : 0.f, sizeof(T) == 2);
+    for (int c = 0; c < D / kWave; ++c) store_out(a.out, row * D + c * kWave + lane, l == 0.f ? 0.f : o[c] / l, sizeof(T) == 2);
     if (lane == 0 && a.lse != nullptr) a.lse[row] = lse_of(m, l);
 }
 
@@ -200,35 +196,41 @@ int most_splits(long long groups, int max_pages, int page) {
     return (int)(want < 1 ? 1 : want > 64 ? 64 : want);
 }
 
-long long row_groups(int b, int n, int Hq, int Hkv) {
-    const int blocks = (Hq / Hkv + kGroupRows - 1) / kGroupRows;
-    return (long long)b * n * Hkv * blocks;
+int row_blocks(int Hq, int Hkv) { return (Hq / Hkv + kGroupRows - 1) / kGroupRows; }
+
+int splits_of(int b, int n, int Hq, int Hkv, int page, int max_pages, bool bf16) {
+    const long long groups = bf16 ? (long long)b * Hkv * tile_blocks(n, Hq, Hkv) : (long long)b * n * Hkv * row_blocks(Hq, Hkv);
+    return most_splits(groups, max_pages, page);
 }
 
-template <class T, int D>
-hipError_t launch_rows(const AttendArgs& a, hipStream_t stream) {
-    const int blocks = (a.Hq / a.Hkv + kGroupRows - 1) / kGroupRows;
-    hipLaunchKernelGGL((attend_rows_kernel<T, D>), dim3(a.b * a.n, a.Hkv * blocks, a.splits), dim3(kAttendThreads), 0,
-                       stream, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    const long long rows = (long long)a.b * a.n * a.Hq;
-    hipLaunchKernelGGL((merge_kernel<T, D>), dim3((unsigned)((rows + kAttendWaves - 1) / kAttendWaves)),
-                       dim3(kAttendThreads), 0, stream, a);
+template <class T>
+hipError_t launch_merge(const AttendArgs& a, int D, hipStream_t stream) {
+    const dim3 grid((unsigned)(((long long)a.b * a.n * a.Hq + kAttendWaves - 1) / kAttendWaves));
+    if (D == 128) hipLaunchKernelGGL((merge_kernel<T, 128>), grid, dim3(kAttendThreads), 0, stream, a);
+    else hipLaunchKernelGGL((merge_kernel<T, 64>), grid, dim3(kAttendThreads), 0, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
 size_t attend_part_bytes(int b, int n, int Hq, int Hkv, int D, int page, int max_pages, bool bf16) {
-    const int splits = most_splits(row_groups(b, n, Hq, Hkv), max_pages, page);
+    const int splits = splits_of(b, n, Hq, Hkv, page, max_pages, bf16);
     return splits == 1 ? 0 : (size_t)splits * b * n * Hq * (D + 2) * 4;
 }
 
 hipError_t launch_tree_attention(AttendArgs a, int D, bool bf16, hipStream_t stream) {
-    a.splits = most_splits(row_groups(a.b, a.n, a.Hq, a.Hkv), a.max_pages, a.page);
-    if (bf16) return D == 128 ? launch_rows<uint16_t, 128>(a, stream) : launch_rows<uint16_t, 64>(a, stream);
-    return D == 128 ? launch_rows<float, 128>(a, stream) : launch_rows<float, 64>(a, stream);
+    a.splits = splits_of(a.b, a.n, a.Hq, a.Hkv, a.page, a.max_pages, bf16);
+    hipError_t e;
+    if (bf16) {
+        e = launch_attend_tile(a, D, stream);
+    } else {
+        const dim3 grid(a.b * a.n, a.Hkv * row_blocks(a.Hq, a.Hkv), a.splits);
+        if (D == 128) hipLaunchKernelGGL(attend_rows_kernel<128>, grid, dim3(kAttendThreads), 0, stream, a);
+        else hipLaunchKernelGGL(attend_rows_kernel<64>, grid, dim3(kAttendThreads), 0, stream, a);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess || a.splits == 1) return e;
+    return bf16 ? launch_merge<uint16_t>(a, D, stream) : launch_merge<float>(a, D, stream);
 }
 
 }  // namespace tf

@@ -34,10 +34,15 @@ __device__ __forceinline__ int new_of(const AttendArgs& a, int s) {
     return a.new_len == nullptr ? a.n : min(max(a.new_len[s], 0), a.n);
 }
 
-// Partials of split contexts: for row r = (s*n + i)*Hq + head and range sp,
-// D sums, then the running maximum (base 2) and the sum of weights.
-__device__ __forceinline__ float* part_of(const AttendArgs& a, size_t row, int sp, int D) {
-    return a.part + ((size_t)sp * a.b * a.n * a.Hq + row) * (D + 2);
+// Partials of split contexts: for row r = (s*n + i)*Hq + head and range sp
+// the D sums, and behind all of them the running maximum (base 2) and the sum
+// of weights.
+__device__ __forceinline__ float* part_sums(const AttendArgs& a, size_t row, int sp, int D) {
+    return a.part + ((size_t)sp * a.b * a.n * a.Hq + row) * D;
+}
+__device__ __forceinline__ float* part_stats(const AttendArgs& a, size_t row, int sp, int D) {
+    const size_t rows = (size_t)a.b * a.n * a.Hq;
+    return a.part + rows * a.splits * D + ((size_t)sp * rows + row) * 2;
 }
 
 __device__ __forceinline__ void store_out(void* out, size_t at, float v, bool bf16) {
@@ -46,6 +51,10 @@ __device__ __forceinline__ void store_out(void* out, size_t at, float v, bool bf
 }
 
 // A finished row: sums over weights (none: zeros and -inf).
-__device__ __forceinline__ float lse_of(float m, float l) { return l > 0.f ? (m + __log2f(l)) * kLn2 : neg_inf(); }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? neg_inf() : (m + __log2f(l)) * kLn2; }
+
+// Blocks of 32 query rows that a key head's positions make.
+int tile_blocks(int n, int Hq, int Hkv);
+hipError_t launch_attend_tile(const AttendArgs& a, int D, hipStream_t stream);
 
 }  // namespace tf

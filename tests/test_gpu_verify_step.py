@@ -395,6 +395,33 @@ def test_attention_rows_without_anything_and_masked_nan(dt):
     check_attention(out, lse, q, kz, vz, mask, [0, 48, 0], i32(table), cache, 0.2)
 
 
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_attention_values_that_are_no_numbers_stay_with_their_rows(dt):
+    """A new position whose key or value is not a number spoils the rows that attend to it, and only those."""
+    rng = np.random.default_rng(20)
+    b, n, Hq, H, D, page, ctx = 2, 41, 4, 2, 128, 16, [70, 0]
+    table, pages, _ = tables(rng, ctx, page, 5)
+    cache = make_cache(rng, pages, H, page, D)
+    q, k, v = (torch.tensor(rng.standard_normal((b, n, h, D))).to(dt).cuda() for h in (Hq, H, H))
+    mask = torch.tensor(tree_masks(rng, b, n)).cuda()
+    kz, vz = k.clone(), v.clone()
+    k[0, 3, 0, 5] = float("nan")
+    v[0, 20, 1, 7], v[1, 40, 0, 9], v[1, 11, 0, 2] = float("nan"), float("-inf"), float("inf")
+    out, lse = binding.treeflash_tree_attention(q, k, v, mask, i32(ctx), i32(table), **cache, scale=0.1)
+    clean, clean_lse = binding.treeflash_tree_attention(q, kz, vz, mask, i32(ctx), i32(table), **cache, scale=0.1)
+    sees = mask.bool()
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[0, :, :2] |= sees[0, :, 3, None, None]
+    hit[0, :, 2:, 7] |= sees[0, :, 20, None]
+    hit[1, :, :2, 9] |= sees[1, :, 40, None]
+    hit[1, :, :2, 2] |= sees[1, :, 11, None]
+    assert torch.equal(~torch.isfinite(out), hit)
+    assert torch.equal(out[~hit], clean[~hit])
+    assert torch.all(torch.isneginf(out[1, 40, :2, 9])) and torch.all(out[1, 11, :2, 2] == float("inf"))
+    spoiled = sees[0, :, 3, None] & (torch.arange(Hq, device="cuda") < 2)
+    assert torch.equal(torch.isnan(lse[0]), spoiled) and torch.equal(lse[1], clean_lse[1])
+
+
 def test_attention_large_products():
     """Products that leave exp's range unless the largest is taken off first, of both signs."""
     rng = np.random.default_rng(17)
