@@ -3,11 +3,24 @@
 //
 // Tokens rank by (logit desc, id asc); every filter keeps a prefix of that
 // order, so the kept set is "keys above a border, and the first few ids of
-// those on it".  Weights are integers: w = rint(2^F exp((z - max)/T)) in 64
-// bits, F = 62 - bits(V), so that sums are exact in any order of additions
-// and a launch's shape cannot change a token.  fp32 sums would not do: a
+// those on it".  Sums are exact far beyond fp32, as integers or in 64 bits: a
 // draw turns on the borders between up to V running sums, and with V errors
-// of 2^-24 one row in a hundred would draw another token.
+// of 2^-24 one row in a hundred would draw another token.  Whatever is added
+// by atomics is an integer, so that the order of additions changes nothing.
+//
+// Two launches.  scan_kernel reads the logits once, a slice of 8192 at a
+// time, and leaves what the row's settings need:
+//   few   (top-k of at most 64, or the largest alone) -- of each 2048 logits
+//         the ones that can be among the row's best k;
+//   whole (else) -- masses of the slice by the value's distance from its
+//         largest, in steps of 1/8.
+// pick_kernel joins a row's slices.  `few` rows are ranked in one wave.  For
+// `whole` rows the steps' masses give each filter's border to one step; the
+// tokens of that step alone are looked up again and ranked, and once the
+// border is known the slices' masses give the slice that the draw falls into,
+// which is walked token by token.  Rows that this cannot serve (an infinite
+// logit, thousands of tokens in the border's step) are read once for each
+// byte of their keys instead (hard_row).
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -16,6 +29,14 @@ namespace tf {
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleWaves = kSampleThreads / kWave;
 constexpr int kSampleTile = 4 * kSampleThreads;   // ids of the draw's first step
+constexpr int kSlice = 8192;                      // logits a workgroup of the scan reads
+constexpr int kScanThreads = 256;
+constexpr int kScanWaves = kScanThreads / kWave;
+constexpr int kChunk = kSlice / kScanWaves;       // of a wave
+constexpr int kFew = 64;                          // tokens that one wave ranks
+constexpr int kList = 128;                        // of a chunk, entries kept
+constexpr int kSteps = 512;                       // of 1/8 below a slice's largest: e^-64 is nothing
+constexpr int kSurvivors = 2048, kBorderList = 4096;
 constexpr uint32_t kKeyNone = 0x007fffffu;        // -inf's key: that and below is no token
 typedef unsigned long long u64;
 
@@ -71,6 +92,25 @@ __device__ __forceinline__ u64 block_before(u64 v, u64* tmp) {
     return before;
 }
 
+// What one sequence asks for.
+struct RowSettings {
+    float t, p, mp;
+    int k;
+    // most tokens a row of them keeps, when that is few (0: it is not)
+    __device__ int few(int V) const {
+        if (!(t > 0.f) || mp > 1.f) return 1;
+        const int n = k > 0 ? min(k, V) : V;
+        return n <= kFew ? n : 0;
+    }
+};
+__device__ __forceinline__ RowSettings settings_of(const SampleArgs& a, int r) {
+    const int s = r / a.n;
+    return {a.temperature != nullptr ? a.temperature[s] : 1.f, a.top_p != nullptr ? a.top_p[s] : 1.f,
+            a.min_p != nullptr ? a.min_p[s] : 0.f, a.top_k != nullptr ? a.top_k[s] : 0};
+}
+// A random number as the draw takes it: within [0, 1 - 2^-24].
+__device__ __forceinline__ double unit(float u) { return u > 0.f ? (double)fminf(u, 0x1.fffffep-1f) : 0.; }
+
 struct Border {
     uint32_t key;      // kept: keys above it
     uint32_t ties;     // and this many of those on it
@@ -124,37 +164,28 @@ __device__ Border find_border(const T* row, int V, const Weigh& w, u64 target, u
     return {};
 }
 
-// A workgroup a row.
+struct HardShared {
+    uint32_t cnt[256];
+    u64 mass[256];
+    u64 tile_mass[(1 << 22) / kSampleTile];
+    uint32_t tile_ties[(1 << 22) / kSampleTile];
+};
+
+// A row whose weights are w = rint(2^bits exp((z - max)/T)) in 64 bits; it has
+// a token, and more than the largest may be kept.
 template <class T>
-__global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a, int bits) {
-    __shared__ uint32_t cnt[256];
-    __shared__ u64 mass[256];
-    __shared__ u64 tmp[kSampleWaves];
-    __shared__ u64 s_state[4];
-    __shared__ u64 tile_mass[(1 << 22) / kSampleTile];
-    __shared__ uint32_t tile_ties[(1 << 22) / kSampleTile];
-    const int tid = threadIdx.x, r = blockIdx.x, s = r / a.n;
+__device__ __noinline__ void hard_row(const SampleArgs& a, const RowSettings& set, uint32_t top, int bits,
+                                      HardShared& sh, u64* tmp, u64* s_state) {
+    uint32_t* cnt = sh.cnt;
+    u64* mass = sh.mass;
+    u64* tile_mass = sh.tile_mass;
+    uint32_t* tile_ties = sh.tile_ties;
+    const int tid = threadIdx.x, r = blockIdx.x;
     const T* row = static_cast<const T*>(a.logits) + (size_t)r * a.ld;
     const int V = a.V;
-    u64 best = 0;
-    for (int i = tid; i < V; i += kSampleThreads) {
-        const u64 k = (u64)key_at(row, i) << 32 | (uint32_t)~i;
-        best = k > best ? k : best;
-    }
-    best = block_max(best, tmp);
-    const uint32_t top = (uint32_t)(best >> 32);
-    const float temp = a.temperature != nullptr ? a.temperature[s] : 1.f;
-    const float mp = a.min_p != nullptr ? a.min_p[s] : 0.f;
-    if (top <= kKeyNone || !(temp > 0.f) || mp > 1.f) {   // no token, or the first one alone
-        if (tid == 0) {
-            a.token[r] = top <= kKeyNone ? -1 : (int)~(uint32_t)best;
-            if (a.logprob != nullptr) a.logprob[r] = top <= kKeyNone ? neg_inf() : 0.f;
-        }
-        return;
-    }
-    const Weigh w{(double)key_f32(top), (double)temp, ldexp(1., bits)};
-    const int k = a.top_k != nullptr ? a.top_k[s] : 0;
-    const float p = a.top_p != nullptr ? a.top_p[s] : 1.f;
+    const Weigh w{(double)key_f32(top), (double)set.t, ldexp(1., bits)};
+    const int k = set.k;
+    const float p = set.p, mp = set.mp;
     Border kept{0, 0, 0};
     bool whole = true;
     if (k > 0 && k < V) {
@@ -200,9 +231,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
             left -= take;
             total += tile_mass[t] + take * tie_w;
         }
-        float u = a.uniform[r];
-        u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-        const u64 target = (u64)((double)u * (double)total);
+        const u64 target = (u64)(unit(a.uniform[r]) * (double)total);
         u64 sum = 0;
         left = kept.ties;
         int t = 0;
@@ -243,13 +272,715 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
     }
 }
 
-size_t sample_ws_bytes(long long rows, int V) { return 0; }
+// ------------------------------------------------------------------ the scan
+
+// What the scan leaves of a slice (workspace, one for each row and slice).
+struct SliceHead {
+    double top;    // whole: step of the slice's largest, rint(8 z / T)
+    float largest; // -inf: no token
+    int used;      // whole: steps that hold anything
+};
+struct ChunkList {
+    float largest;
+    int count;
+    u64 entry[kList];   // key << 32 | ~id
+};
+struct SliceData {
+    SliceHead head;
+    union {
+        struct {
+            u64 mass[kSteps];
+            uint32_t count[kSteps];
+        } whole;
+        ChunkList few[kScanWaves];
+    };
+};
+
+// Vectors of 16 bytes that a lane holds of a chunk; the row is read from the
+// 16-byte boundary at or before its first logit, `skip` logits earlier.
+template <class T>
+struct Chunk {
+    static constexpr int kPer = 16 / sizeof(T);
+    static constexpr int kVecs = kChunk / (kWave * kPer);
+    u32x4 raw[kVecs];
+    __device__ static int skip_of(const T* row) { return (int)(reinterpret_cast<uintptr_t>(row) / sizeof(T) % kPer); }
+    // logits [first, first + kChunk) counted from the boundary; what is no
+    // logit of the row becomes NaN
+    __device__ void load(const T* row, int skip, int V, int first) {
+        const int lane = threadIdx.x & 63, end = V + skip;
+        const u32x4* p = reinterpret_cast<const u32x4*>(row - skip);
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            const int at = first + (i * kWave + lane) * kPer;
+            raw[i] = u32x4{~0u, ~0u, ~0u, ~0u};
+            if (at < end) raw[i] = p[at / kPer];
+        }
+        if (first >= skip && first + kChunk <= end) return;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const int at = first + (i * kWave + lane) * kPer + e;
+                if (at >= skip && at < end) continue;
+                if (sizeof(T) == 4) raw[i][e & 3] = ~0u;
+                else raw[i][(e >> 1) & 3] |= e & 1 ? 0xffff0000u : 0xffffu;
+            }
+    }
+    __device__ float at(int i, int e) const {
+        if (sizeof(T) == 4) return __uint_as_float(raw[i][e & 3]);
+        const uint32_t w = raw[i][(e >> 1) & 3];
+        return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+    }
+};
+
+__device__ __forceinline__ int lanes_below(unsigned long long m) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+
+// The largest t that at least n of the wave's values reach (0: fewer have one).
+__device__ __forceinline__ uint32_t reached_by(uint32_t key, int n) {
+    uint32_t t = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t up = t | 1u << bit;
+        if (__popcll(__ballot(key >= up)) >= n) t = up;
+    }
+    return t;
+}
+
+// A wave's chunk: the logits among which its n best are.  The n-th largest of
+// the lanes' own largest is a bound that at least n logits reach, and in a
+// chunk without order few more do; a chunk in which too many do is searched
+// for its n-th largest itself.
+template <class T>
+__device__ void scan_few(const Chunk<T>& c, int first, int skip, int n, ChunkList* out) {
+    constexpr int kPer = Chunk<T>::kPer, kVecs = Chunk<T>::kVecs;
+    const int lane = threadIdx.x & 63;
+    float mx = neg_inf();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) mx = fmaxf(mx, c.at(i, e));   // NaN is passed over
+    const uint32_t bound = reached_by(logit_key(mx), n);
+    const float least = bound > kKeyNone ? key_f32(bound) : -__FLT_MAX__;   // -inf is no token
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) count += __popcll(__ballot(c.at(i, e) >= least));
+    mx = wave_max(mx);
+    if (count <= kList) {
+        int at = 0;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const float z = c.at(i, e);
+                const unsigned long long m = __ballot(z >= least);
+                if (m == 0) continue;
+                if (z >= least)
+                    out->entry[at + lanes_below(m)] = (u64)logit_key(z) << 32 | (uint32_t)~(first - skip + (i * kWave + lane) * kPer + e);
+                at += __popcll(m);
+            }
+    } else {
+        uint32_t t = 0;   // the n-th largest key
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t up = t | 1u << bit;
+            int reach = 0;
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) reach += __popcll(__ballot(logit_key(c.at(i, e)) >= up));
+            if (reach >= n) t = up;
+        }
+        int at = 0;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const uint32_t key = logit_key(c.at(i, e));
+                const unsigned long long m = __ballot(key > t);
+                if (key > t) out->entry[at + lanes_below(m)] = (u64)key << 32 | (uint32_t)~(first - skip + (i * kWave + lane) * kPer + e);
+                at += __popcll(m);
+            }
+        // of those equal to it the first by id: a vector's lanes hold ids in order
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            int mine = 0;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) mine += logit_key(c.at(i, e)) == t ? 1 : 0;
+            int before = mine;
+            for (int o = 1; o < 64; o <<= 1) {
+                const int up = __shfl_up(before, o);
+                if (lane >= o) before += up;
+            }
+            const int all = __shfl(before, 63);
+            int slot = at + before - mine;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (logit_key(c.at(i, e)) == t) {
+                    if (slot < n) out->entry[slot] = (u64)t << 32 | (uint32_t)~(first - skip + (i * kWave + lane) * kPer + e);
+                    ++slot;
+                }
+            at = min(n, at + all);
+        }
+        count = at;
+    }
+    if (lane == 0) {
+        out->largest = mx;
+        out->count = count;
+    }
+}
+
+// Where a logit lies: y = 8 z / T, its step rint(y) and exp of what is left,
+// |rest| <= 1/16, by its series to the 7th power (error 2^-47).
+// The product is rounded before the step is taken off: fused with the
+// difference it would give a large y's rounding error for its rest.
+struct Step {
+    double step, rest;
+};
+__device__ __forceinline__ double steps_at(float z, double per) {
+#pragma clang fp contract(off)
+    return (double)z * per;
+}
+__device__ __forceinline__ Step step_of(float z, double per) {
+    const double y = steps_at(z, per), b = rint(y);
+    return {b, y - b};
+}
+__device__ __forceinline__ double exp_rest(double r) {
+    const double x = r * 0.125;
+    double s = 1. / 5040;
+    s = fma(s, x, 1. / 720);
+    s = fma(s, x, 1. / 120);
+    s = fma(s, x, 1. / 24);
+    s = fma(s, x, 1. / 6);
+    s = fma(s, x, 0.5);
+    s = fma(s, x, 1.);
+    return fma(s, x, 1.);
+}
+// exp of the rest as an integer, 2^bits the one (bits <= 48): rounded by the
+// addition of 2^52, whose sum holds it in the low bits
+__device__ __forceinline__ u64 fixed_rest(double r, double one) {
+    return (u64)__double_as_longlong(fma(exp_rest(r), one, 0x1p52)) & ((1ull << 52) - 1);
+}
+
+struct ScanShared {
+    u64 mass[kSteps];
+    uint32_t count[kSteps];
+    float top[kScanWaves];
+    int used;
+};
+
+// A slice's masses by step.  What it costs is fp64 arithmetic (a dozen
+// operations a logit, at fp32's rate here) and one LDS atomic.
+template <class T>
+__device__ void scan_whole(const Chunk<T>& c, const RowSettings& set, double one, ScanShared& sh, SliceData* out) {
+    constexpr int kPer = Chunk<T>::kPer, kVecs = Chunk<T>::kVecs;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int j = tid; j < kSteps; j += kScanThreads) sh.mass[j] = 0, sh.count[j] = 0;
+    if (tid == 0) sh.used = 0;
+    float mx = neg_inf();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) mx = fmaxf(mx, c.at(i, e));
+    mx = wave_max(mx);
+    if (lane == 0) sh.top[wave] = mx;
+    __syncthreads();
+    for (int w = 0; w < kScanWaves; ++w) mx = fmaxf(mx, sh.top[w]);
+    const double per = 8. / (double)set.t;
+    const double top = step_of(mx, per).step;
+    const bool counted = set.k > 0;
+    int last = -1;
+    if (mx > neg_inf()) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const Step s = step_of(c.at(i, e), per);
+                const double d = top - s.step;
+                if (d < (double)kSteps) {   // neither NaN nor -inf
+                    const int j = (int)d;
+                    last = max(last, j);
+                    atomicAdd(&sh.mass[j], fixed_rest(s.rest, one));
+                    if (counted) atomicAdd(&sh.count[j], 1u);
+                }
+            }
+    }
+    atomicMax(&sh.used, last + 1);
+    __syncthreads();
+    const int used = sh.used;
+    for (int j = tid; j < used; j += kScanThreads) {
+        out->whole.mass[j] = sh.mass[j];
+        if (counted) out->whole.count[j] = sh.count[j];
+    }
+    if (tid == 0) out->head = {top, mx, used};
+}
+
+// Workgroup (slice, row).
+template <class T>
+__global__ __launch_bounds__(kScanThreads) void scan_kernel(SampleArgs a, int bits) {
+    __shared__ ScanShared sh;
+    const int r = blockIdx.y * 32768 + blockIdx.z, wave = threadIdx.x >> 6;
+    if (r >= a.rows) return;
+    const T* row = static_cast<const T*>(a.logits) + (size_t)r * a.ld;
+    const int skip = Chunk<T>::skip_of(row);
+    const int first = blockIdx.x * kSlice + wave * kChunk;
+    SliceData* out = reinterpret_cast<SliceData*>(a.ws) + (size_t)r * gridDim.x + blockIdx.x;
+    const RowSettings set = settings_of(a, r);
+    Chunk<T> c;
+    c.load(row, skip, a.V, first);
+    const int n = set.few(a.V);
+    if (n > 0) scan_few(c, first, skip, n, &out->few[wave]);
+    else scan_whole(c, set, ldexp(1., bits), sh, out);
+}
+
+// ------------------------------------------------------------------ the pick
+
+// 64 values, a lane each, sorted with the largest in lane 0.
+__device__ __forceinline__ u64 wave_sort(u64 v) {
+    const int lane = threadIdx.x & 63;
+    for (int size = 2; size <= 64; size <<= 1)
+        for (int j = size >> 1; j > 0; j >>= 1) {
+            const u64 w = __shfl_xor(v, j);
+            const bool low = (lane & j) == 0, down = (lane & size) == 0;   // this lane takes the larger
+            v = (low == down) == (v > w) ? v : w;
+        }
+    return v;
+}
+// The 64 largest of two such lists, sorted.
+__device__ __forceinline__ u64 wave_merge(u64 a, u64 b) {
+    const int lane = threadIdx.x & 63;
+    const u64 r = __shfl(b, 63 - lane);
+    u64 v = a > r ? a : r;
+    for (int j = 32; j > 0; j >>= 1) {
+        const u64 w = __shfl_xor(v, j);
+        v = ((lane & j) == 0) == (v > w) ? v : w;
+    }
+    return v;
+}
+
+struct FewShared {
+    u64 list[kSurvivors];
+    int count;
+};
+
+// The draw from at most 64 ranked tokens, in one wave.
+__device__ void draw_few(const SampleArgs& a, const RowSettings& set, u64 best, int n, int bits) {
+    const int lane = threadIdx.x & 63, r = blockIdx.x;
+    const uint32_t key = (uint32_t)(best >> 32);
+    const int id = (int)~(uint32_t)best;
+    const u64 real = __ballot(lane < n && key > kKeyNone);
+    n = __popcll(real);
+    if (n == 0) {
+        if (lane == 0) {
+            a.token[r] = -1;
+            if (a.logprob != nullptr) a.logprob[r] = neg_inf();
+        }
+        return;
+    }
+    const bool first = !(set.t > 0.f) || set.mp > 1.f;
+    const Weigh w{(double)key_f32((uint32_t)__shfl((int)key, 0)), (double)set.t, ldexp(1., bits)};
+    u64 x = first ? (u64)(lane == 0) << bits : lane < n ? w.weight(key) : 0ull;
+    if (first) n = 1;
+    u64 c = x;
+    for (int o = 1; o < 64; o <<= 1) {
+        const u64 up = __shfl_up(c, o);
+        if (lane >= o) c += up;
+    }
+    if (set.p < 1.f && !first) {
+        const double want = ceil((double)set.p * (double)__shfl(c, 63));
+        n = min(n, __popcll(__ballot(lane < n && (double)c < want)) + 1);
+    }
+    if (set.mp > 0.f && !first) n = max(1, min(n, __popcll(__ballot(lane < n && exp(w.power(key)) >= (double)set.mp))));
+    const u64 total = __shfl(c, n - 1);
+    const u64 target = (u64)(unit(a.uniform[r]) * (double)total);
+    u64 before = 0;   // of the kept with a lower id
+    for (int o = 0; o < n; ++o) {
+        const int other = __shfl(id, o);
+        const u64 xo = __shfl(x, o);
+        before += other < id ? xo : 0ull;
+    }
+    if (lane < n && before <= target && target < before + x) {
+        a.token[r] = id;
+        if (a.logprob != nullptr) a.logprob[r] = first ? 0.f : (float)(w.power(key) - log((double)total / w.one));
+    }
+}
+
+// Joins a row's lists.  The n-th largest of the lanes' largest list heads
+// bounds what can be among the best n; those survivors are ranked by one wave,
+// 64 at a time.  Returns false where too many survive.
+__device__ bool pick_few(const SampleArgs& a, const RowSettings& set, const SliceData* data, int slices, int n,
+                         int bits, FewShared& sh, u64* tmp) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int lists = slices * kScanWaves;
+    if (n == 1) {
+        u64 best = 0;
+        for (int i = wave; i < lists; i += kSampleWaves) {
+            const ChunkList& l = data[i / kScanWaves].few[i % kScanWaves];
+            for (int e = lane; e < l.count; e += kWave) best = l.entry[e] > best ? l.entry[e] : best;
+        }
+        best = block_max(best, tmp);
+        if (wave == 0) draw_few(a, set, lane == 0 ? best : 0ull, 1, bits);
+        return true;
+    }
+    float mx = neg_inf();
+    for (int i = lane; i < lists; i += kWave) mx = fmaxf(mx, data[i / kScanWaves].few[i % kScanWaves].largest);
+    const uint32_t bound = reached_by(logit_key(mx), n);
+    if (tid == 0) sh.count = 0;
+    __syncthreads();
+    for (int i = wave; i < lists; i += kSampleWaves) {
+        const ChunkList& l = data[i / kScanWaves].few[i % kScanWaves];
+        const int count = l.count;
+        for (int e = lane; e < count; e += kWave) {
+            const u64 x = l.entry[e];
+            if ((uint32_t)(x >> 32) < bound) continue;
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < kSurvivors) sh.list[at] = x;
+        }
+    }
+    __syncthreads();
+    const int count = sh.count;
+    if (count > kSurvivors) return false;
+    if (wave == 0) {
+        u64 best = 0;
+        for (int i = 0; i < count; i += kWave) best = wave_merge(best, wave_sort(i + lane < count ? sh.list[i + lane] : 0ull));
+        draw_few(a, set, best, n, bits);
+    }
+    return true;
+}
+
+constexpr int kMaxSlices = ((1 << 22) + kSlice - 1) / kSlice + 1;
+
+struct WholeShared {
+    u64 mass[kSteps];
+    uint32_t count[kSteps];
+    double upto[kSteps];      // mass of steps 0..j, the largest logit's weight being 1
+    double unit[kSteps];      // weight of a step's middle
+    u64 list[kBorderList];    // the border's step: key << 32 | ~id, ranked
+    u64 border[kMaxSlices];   // kept mass of that step, by slice
+    double slice[kMaxSlices];
+    int listed, cut, pick, last;
+};
+
+// Inclusive sum of one double a thread, in a fixed order.
+__device__ __forceinline__ double block_upto(double v, double* tmp) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int o = 1; o < 64; o <<= 1) {
+        const double up = __shfl_up(v, o);
+        if (lane >= o) v += up;
+    }
+    if (lane == 63) tmp[wave] = v;
+    __syncthreads();
+    double before = 0.;
+    for (int w = 0; w < wave; ++w) before += tmp[w];
+    __syncthreads();
+    return before + v;
+}
+
+// Smallest value over the workgroup.
+__device__ __forceinline__ int block_min(int v, int* cell) {
+    if (threadIdx.x == 0) *cell = 0x7fffffff;
+    __syncthreads();
+    if (v != 0x7fffffff) atomicMin(cell, v);
+    __syncthreads();
+    v = *cell;
+    __syncthreads();
+    return v;
+}
+
+template <class T>
+struct Whole {
+    const SampleArgs& a;
+    const RowSettings& set;
+    const SliceData* data;
+    WholeShared& sh;
+    u64* tmp;
+    const T* row;
+    int slices, skip, r;
+    double per, top, ytop, one;
+    float largest;
+
+    __device__ int step_below(const SliceHead& h) const {   // steps from the row's top to the slice's
+        const double d = top - h.top;
+        return d < (double)kSteps ? (int)d : kSteps;
+    }
+    // Ranks the tokens of step j; false where they are too many.
+    __device__ bool rank_step(int j) {
+        const int tid = threadIdx.x;
+        constexpr int kPer = Chunk<T>::kPer;
+        if (tid == 0) sh.listed = 0;
+        __syncthreads();
+        for (int s = 0; s < slices; ++s) {
+            const SliceHead h = data[s].head;
+            const int at = j - step_below(h);
+            if (!(h.largest > neg_inf()) || at < 0 || at >= h.used || data[s].whole.mass[at] == 0) continue;   // uniform
+            const int end = min((s + 1) * kSlice, a.V + skip);
+            for (int v = s * kSlice + tid * kPer; v < end; v += kSampleThreads * kPer) {
+                const u32x4 raw = *reinterpret_cast<const u32x4*>(row - skip + v);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    float z;
+                    if (sizeof(T) == 4) z = __uint_as_float(raw[e & 3]);
+                    else z = __uint_as_float(e & 1 ? raw[(e >> 1) & 3] & 0xffff0000u : raw[(e >> 1) & 3] << 16);
+                    if (v + e < skip || v + e >= end || !(top - step_of(z, per).step == (double)j)) continue;
+                    const int slot = atomicAdd(&sh.listed, 1);
+                    if (slot < kBorderList) sh.list[slot] = (u64)logit_key(z) << 32 | (uint32_t)~(v + e - skip);
+                }
+            }
+        }
+        __syncthreads();
+        const int n = sh.listed;
+        if (n > kBorderList) return false;
+        int size = 2;
+        while (size < n) size <<= 1;
+        for (int i = n + tid; i < size; i += kSampleThreads) sh.list[i] = 0;
+        __syncthreads();
+        for (int k = 2; k <= size; k <<= 1)
+            for (int m = k >> 1; m > 0; m >>= 1) {
+                for (int i = tid; i < size / 2; i += kSampleThreads) {
+                    const int lo = (i / m) * 2 * m + i % m, hi = lo + m;
+                    const u64 x = sh.list[lo], y = sh.list[hi];
+                    if (((lo & k) == 0) == (x < y)) sh.list[lo] = y, sh.list[hi] = x;
+                }
+                __syncthreads();
+            }
+        return true;
+    }
+    __device__ u64 listed_weight(int i) const { return fixed_rest(step_of(key_f32((uint32_t)(sh.list[i] >> 32)), per).rest, one); }
+    // Weights of the ranked step's first `n` tokens, and how many of them it
+    // takes to reach `target` of them (n if all together do not).
+    __device__ double ranked_mass(int n, double target, int* reach) {
+        constexpr int kPer = kBorderList / kSampleThreads;
+        const int tid = threadIdx.x;
+        u64 x[kPer], sum = 0;
+        for (int e = 0; e < kPer; ++e) {
+            const int i = tid * kPer + e;
+            x[e] = i < n ? listed_weight(i) : 0ull;
+            sum += x[e];
+        }
+        u64 at = block_before(sum, tmp);
+        const u64 all = block_sum(sum);
+        int found = 0x7fffffff;
+        for (int e = 0; e < kPer; ++e) {
+            at += x[e];
+            if (found == 0x7fffffff && tid * kPer + e < n && (double)at >= target) found = tid * kPer + e;
+        }
+        found = block_min(found, &sh.cut);
+        if (reach != nullptr) *reach = found < n ? found + 1 : n;
+        return (double)all;
+    }
+    __device__ u64 block_sum(u64 v) {
+        const u64 before = block_before(v, tmp);
+        if (threadIdx.x == kSampleThreads - 1) tmp[0] = before + v;
+        __syncthreads();
+        const u64 all = tmp[0];
+        __syncthreads();
+        return all;
+    }
+
+    // Draws the row's token; false where the row is to be read byte by byte.
+    __device__ bool draw() {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        for (int j = tid; j < kSteps; j += kSampleThreads) {
+            sh.mass[j] = 0;
+            sh.count[j] = 0;
+        }
+        for (int s = tid; s < slices; s += kSampleThreads) sh.border[s] = 0;
+        __syncthreads();
+        const bool counted = set.k > 0;
+        for (int s = wave; s < slices; s += kSampleWaves) {
+            const SliceHead h = data[s].head;
+            const int below = h.largest > neg_inf() ? step_below(h) : kSteps;
+            for (int j = lane; j < h.used && j + below < kSteps; j += kWave) {
+                const u64 m = data[s].whole.mass[j];
+                if (m != 0) atomicAdd(&sh.mass[j + below], m);
+                if (counted && m != 0) atomicAdd(&sh.count[j + below], data[s].whole.count[j]);
+            }
+        }
+        __syncthreads();
+        // thread j < kSteps is step j
+        const double weight = tid < kSteps ? exp(((top - ytop) - (double)tid) * 0.125) / one : 0.;
+        const double upto = block_upto(tid < kSteps ? (double)sh.mass[tid] * weight : 0., reinterpret_cast<double*>(tmp));
+        if (tid < kSteps) sh.unit[tid] = weight, sh.upto[tid] = upto;
+        __syncthreads();
+        // the kept: steps above `edge` whole, of that one the first `part` ranked tokens
+        int edge = kSteps, part = 0, ranked = -1;
+        double total = sh.upto[kSteps - 1];
+        if (counted && set.k < a.V) {
+            const u64 n = block_before(tid < kSteps ? sh.count[tid] : 0u, tmp);
+            const int j = block_min(tid < kSteps && n + sh.count[tid] >= (u64)set.k ? tid : 0x7fffffff, &sh.cut);
+            if (j < kSteps) {
+                if (tid == j) sh.cut = set.k - (int)n;
+                __syncthreads();
+                part = sh.cut;
+                __syncthreads();
+                if (!rank_step(j)) return false;
+                edge = ranked = j;
+                total = (j > 0 ? sh.upto[j - 1] : 0.) + ranked_mass(part, 0., nullptr) * sh.unit[j];
+            }
+        }
+        if (set.p < 1.f) {
+            const double target = (double)set.p * total;
+            int j = block_min(tid < min(edge + 1, kSteps) && sh.upto[min(tid, kSteps - 1)] >= target ? tid : 0x7fffffff, &sh.cut);
+            if (j == 0x7fffffff && edge < kSteps) j = edge;   // the border's own rounding
+            if (j < kSteps) {
+                const double above = j > 0 ? sh.upto[j - 1] : 0.;
+                if (j != ranked) {
+                    if (!rank_step(j)) return false;
+                    ranked = j;
+                    part = sh.listed;
+                }
+                edge = j;
+                const int most = part;
+                ranked_mass(most, (target - above) / sh.unit[j], &part);
+                total = above + ranked_mass(part, 0., nullptr) * sh.unit[j];
+            }
+        }
+        if (set.mp > 0.f) {
+            const double least = (double)set.mp;
+            const double d = top - rint(ytop + 8. * log(least));
+            const int j = d < (double)kSteps ? (int)d : kSteps;
+            if (j <= edge && j < kSteps) {
+                if (j != ranked) {
+                    if (!rank_step(j)) return false;
+                    ranked = j;
+                    part = sh.listed;
+                }
+                edge = j;
+                int n = 0;
+                for (int i = tid; i < part; i += kSampleThreads) {
+                    const double x = ((double)key_f32((uint32_t)(sh.list[i] >> 32)) - (double)largest) / (double)set.t;
+                    n += exp(x) >= least ? 1 : 0;
+                }
+                part = (int)block_sum((u64)n);
+                total = (j > 0 ? sh.upto[j - 1] : 0.) + ranked_mass(part, 0., nullptr) * sh.unit[j];
+            }
+        }
+        const u64 least = part > 0 ? sh.list[part - 1] : ~0ull;   // of the edge's step, what ranks no later
+        for (int i = tid; i < part; i += kSampleThreads)
+            atomicAdd(&sh.border[((int)~(uint32_t)sh.list[i] + skip) / kSlice], listed_weight(i));
+        if (tid == 0) sh.pick = 0x7fffffff, sh.last = -1;
+        __syncthreads();
+        for (int s = wave; s < slices; s += kSampleWaves) {
+            const SliceHead h = data[s].head;
+            const int below = h.largest > neg_inf() ? step_below(h) : kSteps;
+            double m = 0.;
+            for (int j = lane; j < h.used && j + below < edge; j += kWave) m += (double)data[s].whole.mass[j] * sh.unit[j + below];
+            for (int o = 32; o > 0; o >>= 1) m += __shfl_xor(m, o);
+            if (lane == 0) sh.slice[s] = m + (edge < kSteps ? (double)sh.border[s] * sh.unit[edge] : 0.);
+        }
+        __syncthreads();
+        // every thread finds the slice: the first whose running sum exceeds
+        // the target, or by rounding the last that holds anything
+        const double target = unit(a.uniform[r]) * total;
+        double before = 0.;
+        int at = 0;
+        double sum = 0.;
+        for (int s = 0; s < slices; ++s) {
+            const double m = sh.slice[s];
+            if (m > 0.) {
+                at = s;
+                before = sum;
+            }
+            sum += m;
+            if (m > 0. && sum > target) break;
+        }
+        constexpr int kEach = kSlice / kSampleThreads;
+        double w[kEach], mine = 0.;
+        for (int e = 0; e < kEach; ++e) {
+            const int v = at * kSlice + tid * kEach + e;
+            w[e] = 0.;
+            if (v < skip || v >= a.V + skip) continue;
+            const uint32_t key = key_at(row, v - skip);
+            if (key <= kKeyNone) continue;
+            const Step st = step_of(key_f32(key), per);
+            const double d = top - st.step;
+            if (!(d < (double)kSteps) || (int)d > edge) continue;
+            if ((int)d == edge && ((u64)key << 32 | (uint32_t)~(v - skip)) < least) continue;
+            w[e] = (double)fixed_rest(st.rest, one) * sh.unit[(int)d];
+            mine += w[e];
+        }
+        double run = before + block_upto(mine, reinterpret_cast<double*>(tmp)) - mine;
+        for (int e = 0; e < kEach; ++e) {
+            const int v = at * kSlice + tid * kEach + e;
+            run += w[e];
+            if (w[e] > 0.) {
+                atomicMax(&sh.last, v);
+                if (run > target) atomicMin(&sh.pick, v);
+            }
+        }
+        __syncthreads();
+        if (tid == 0) {
+            const int v = (sh.pick != 0x7fffffff ? sh.pick : sh.last) - skip;
+            a.token[r] = v;
+            if (a.logprob != nullptr)
+                a.logprob[r] = (float)(((double)key_f32(key_at(row, v)) - (double)largest) / (double)set.t - log(total));
+        }
+        return true;
+    }
+};
+
+// A workgroup a row.
+template <class T>
+__global__ __launch_bounds__(kSampleThreads) void pick_kernel(SampleArgs a, int slices, int bits) {
+    __shared__ union {
+        FewShared few;
+        WholeShared whole;
+        HardShared hard;
+    } sh;
+    __shared__ u64 tmp[kSampleWaves];
+    __shared__ u64 s_state[4];
+    const int r = blockIdx.x, lane = threadIdx.x & 63;
+    const SliceData* data = reinterpret_cast<const SliceData*>(a.ws) + (size_t)r * slices;
+    const RowSettings set = settings_of(a, r);
+    const int n = set.few(a.V);
+    float largest = neg_inf();
+    if (n > 0) {
+        if (pick_few(a, set, data, slices, n, bits, sh.few, tmp)) return;
+        for (int i = lane; i < slices * kScanWaves; i += kWave)
+            largest = fmaxf(largest, data[i / kScanWaves].few[i % kScanWaves].largest);
+    } else {
+        for (int i = lane; i < slices; i += kWave) largest = fmaxf(largest, data[i].head.largest);
+    }
+    largest = wave_max(largest);
+    if (n == 0) {
+        if (largest == neg_inf()) {
+            if (threadIdx.x == 0) {
+                a.token[r] = -1;
+                if (a.logprob != nullptr) a.logprob[r] = neg_inf();
+            }
+            return;
+        }
+        if (largest < __builtin_inff()) {
+            const T* row = static_cast<const T*>(a.logits) + (size_t)r * a.ld;
+            const double per = 8. / (double)set.t;
+            Whole<T> w{a, set, data, sh.whole, tmp, row, slices, Chunk<T>::skip_of(row), r, per,
+                       step_of(largest, per).step, steps_at(largest, per), ldexp(1., bits), largest};
+            if (w.draw()) return;
+        }
+    }
+    __syncthreads();
+    hard_row<T>(a, set, logit_key(largest), bits, sh.hard, tmp, s_state);
+}
+
+namespace {
+int slices_of(int V) { return (V + 7 + kSlice - 1) / kSlice; }   // a row may begin up to 7 logits behind a boundary
+}
+
+size_t sample_ws_bytes(long long rows, int V) { return (size_t)rows * slices_of(V) * sizeof(SliceData); }
 
 hipError_t launch_sample(const SampleArgs& a, bool bf16, hipStream_t stream) {
-    int bits = 62;
+    int bits = 62;   // sums of V weights of at most 1.07 * 2^bits stay below 2^63
     for (int v = a.V; v > 0; v >>= 1) --bits;
-    if (bf16) hipLaunchKernelGGL(sample_row_kernel<uint16_t>, dim3(a.rows), dim3(kSampleThreads), 0, stream, a, bits);
-    else hipLaunchKernelGGL(sample_row_kernel<float>, dim3(a.rows), dim3(kSampleThreads), 0, stream, a, bits);
+    bits = bits < 48 ? bits : 48;
+    const int slices = slices_of(a.V);
+    const dim3 grid(slices, (a.rows - 1) / 32768 + 1, a.rows < 32768 ? a.rows : 32768);
+    if (bf16) hipLaunchKernelGGL(scan_kernel<uint16_t>, grid, dim3(kScanThreads), 0, stream, a, bits);
+    else hipLaunchKernelGGL(scan_kernel<float>, grid, dim3(kScanThreads), 0, stream, a, bits);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (bf16) hipLaunchKernelGGL(pick_kernel<uint16_t>, dim3(a.rows), dim3(kSampleThreads), 0, stream, a, slices, bits);
+    else hipLaunchKernelGGL(pick_kernel<float>, dim3(a.rows), dim3(kSampleThreads), 0, stream, a, slices, bits);
     return hipGetLastError();
 }
 
