@@ -353,7 +353,8 @@ size_t treeflash_sample_workspace_bytes(int b, int n, int V);
 /* A token for each of n positions of b sequences, from given random numbers.
  *   logits       rows of V values (dtype dt); row r = s*n + i starts at element r*ld,
  *                ld >= V (any alignment of the element size)
- *   temperature  [b] fp32 or NULL (1): 0 (or below, or NaN) takes the largest logit
+ *   temperature  [b] fp32 or NULL (1): 0 (or below, or NaN) takes the largest logit;
+ *                above 1e30 counts as 1e30
  *   top_k        [b] int32 or NULL: <= 0 or >= V is off
  *   top_p        [b] fp32 or NULL: >= 1 or NaN is off
  *   min_p        [b] fp32 or NULL: <= 0 or NaN is off

@@ -26,7 +26,7 @@
 
 namespace tf {
 
-constexpr int kSampleThreads = 1024;
+constexpr int kSampleThreads = 512;
 constexpr int kSampleWaves = kSampleThreads / kWave;
 constexpr int kSampleTile = 4 * kSampleThreads;   // ids of the draw's first step
 constexpr int kSlice = 8192;                      // logits a workgroup of the scan reads
@@ -105,7 +105,9 @@ struct RowSettings {
 };
 __device__ __forceinline__ RowSettings settings_of(const SampleArgs& a, int r) {
     const int s = r / a.n;
-    return {a.temperature != nullptr ? a.temperature[s] : 1.f, a.top_p != nullptr ? a.top_p[s] : 1.f,
+    const float t = a.temperature != nullptr ? a.temperature[s] : 1.f;
+    // beyond 1e30 the weights are flat already, and z / T must not become 0 * inf
+    return {t > 0.f ? fminf(t, 1e30f) : 0.f, a.top_p != nullptr ? a.top_p[s] : 1.f,
             a.min_p != nullptr ? a.min_p[s] : 0.f, a.top_k != nullptr ? a.top_k[s] : 0};
 }
 // A random number as the draw takes it: within [0, 1 - 2^-24].
@@ -276,9 +278,10 @@ __device__ __noinline__ void hard_row(const SampleArgs& a, const RowSettings& se
 
 // What the scan leaves of a slice (workspace, one for each row and slice).
 struct SliceHead {
-    double top;    // whole: step of the slice's largest, rint(8 z / T)
-    float largest; // -inf: no token
+    int top;       // whole: step of the slice's largest
     int used;      // whole: steps that hold anything
+    float largest; // -inf: no token
+    int unused;
 };
 struct ChunkList {
     float largest;
@@ -431,37 +434,42 @@ __device__ void scan_few(const Chunk<T>& c, int first, int skip, int n, ChunkLis
     }
 }
 
-// Where a logit lies: y = 8 z / T, its step rint(y) and exp of what is left,
-// |rest| <= 1/16, by its series to the 7th power (error 2^-47).
-// The product is rounded before the step is taken off: fused with the
-// difference it would give a large y's rounding error for its rest.
+// Where a logit lies: y = 8 z / T, its step b (the nearest integer) and exp of
+// what is left, |rest| <= 1/16, by its series to the 7th power (error 2^-47).
+// Adding 1.5 * 2^52 rounds to an integer and leaves it in the sum's low bits,
+// which takes three operations for step and rest.  Rows whose largest |y| is
+// 2^20 or more (kFar) are left to hard_row: there a step is no longer far
+// above the logits' own rounding.
+constexpr double kRound = 0x1.8p52;
+constexpr double kFar = 0x1p20;
 struct Step {
-    double step, rest;
+    int step;
+    double rest;   // of y
 };
-__device__ __forceinline__ double steps_at(float z, double per) {
-#pragma clang fp contract(off)
-    return (double)z * per;
-}
 __device__ __forceinline__ Step step_of(float z, double per) {
-    const double y = steps_at(z, per), b = rint(y);
-    return {b, y - b};
+    const double t = fma((double)z, per, kRound), b = t - kRound;
+    return {(int)(uint32_t)__double_as_longlong(t), fma((double)z, per, -b)};
 }
-__device__ __forceinline__ double exp_rest(double r) {
-    const double x = r * 0.125;
-    double s = 1. / 5040;
-    s = fma(s, x, 1. / 720);
-    s = fma(s, x, 1. / 120);
-    s = fma(s, x, 1. / 24);
-    s = fma(s, x, 1. / 6);
-    s = fma(s, x, 0.5);
-    s = fma(s, x, 1.);
-    return fma(s, x, 1.);
-}
-// exp of the rest as an integer, 2^bits the one (bits <= 48): rounded by the
-// addition of 2^52, whose sum holds it in the low bits
-__device__ __forceinline__ u64 fixed_rest(double r, double one) {
-    return (u64)__double_as_longlong(fma(exp_rest(r), one, 0x1p52)) & ((1ull << 52) - 1);
-}
+// exp(rest / 8) as an integer, 2^bits the one (bits <= 48): the coefficients
+// carry that factor, and a constant term 2^52 more rounds the sum and leaves
+// the integer in its low bits.
+struct Series {
+    double c[8];
+    __device__ explicit Series(double one) {
+        double f = one;
+        for (int n = 0; n < 8; ++n) {
+            c[n] = f;
+            f *= 0.125 / (n + 1);
+        }
+        c[0] += 0x1p52;
+    }
+    __device__ u64 operator()(double r) const {
+        double s = c[7];
+#pragma unroll
+        for (int n = 6; n >= 0; --n) s = fma(s, r, c[n]);
+        return (u64)__double_as_longlong(s) & ((1ull << 52) - 1);
+    }
+};
 
 struct ScanShared {
     u64 mass[kSteps];
@@ -488,20 +496,22 @@ __device__ void scan_whole(const Chunk<T>& c, const RowSettings& set, double one
     __syncthreads();
     for (int w = 0; w < kScanWaves; ++w) mx = fmaxf(mx, sh.top[w]);
     const double per = 8. / (double)set.t;
-    const double top = step_of(mx, per).step;
     const bool counted = set.k > 0;
-    int last = -1;
-    if (mx > neg_inf()) {
+    int last = -1, top = 0;
+    if (mx > neg_inf() && fabs((double)mx * per) < kFar) {
+        top = step_of(mx, per).step;
+        // what lies further down, -inf and NaN stop just outside the steps
+        const float least = (float)((top - (kSteps + 8)) / per);
+        const Series weight(one);
 #pragma unroll
         for (int i = 0; i < kVecs; ++i)
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
-                const Step s = step_of(c.at(i, e), per);
-                const double d = top - s.step;
-                if (d < (double)kSteps) {   // neither NaN nor -inf
-                    const int j = (int)d;
+                const Step s = step_of(fmaxf(c.at(i, e), least), per);
+                const int j = top - s.step;
+                if (j < kSteps) {
                     last = max(last, j);
-                    atomicAdd(&sh.mass[j], fixed_rest(s.rest, one));
+                    atomicAdd(&sh.mass[j], weight(s.rest));
                     if (counted) atomicAdd(&sh.count[j], 1u);
                 }
             }
@@ -513,7 +523,7 @@ __device__ void scan_whole(const Chunk<T>& c, const RowSettings& set, double one
         out->whole.mass[j] = sh.mass[j];
         if (counted) out->whole.count[j] = sh.count[j];
     }
-    if (tid == 0) out->head = {top, mx, used};
+    if (tid == 0) out->head = {top, used, mx, 0};
 }
 
 // Workgroup (slice, row).
@@ -536,12 +546,22 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(SampleArgs a, int bi
 
 // ------------------------------------------------------------------ the pick
 
+__device__ __forceinline__ u64 lane_xor64(u64 v, int j) {
+    return (u64)(uint32_t)lane_xor_n((int)(v >> 32), j) << 32 | (uint32_t)lane_xor_n((int)v, j);
+}
+// The value of one lane, the same for the whole wave.
+__device__ __forceinline__ u64 lane_value(u64 v, int lane) {
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
 // 64 values, a lane each, sorted with the largest in lane 0.
 __device__ __forceinline__ u64 wave_sort(u64 v) {
     const int lane = threadIdx.x & 63;
+#pragma unroll
     for (int size = 2; size <= 64; size <<= 1)
+#pragma unroll
         for (int j = size >> 1; j > 0; j >>= 1) {
-            const u64 w = __shfl_xor(v, j);
+            const u64 w = lane_xor64(v, j);
             const bool low = (lane & j) == 0, down = (lane & size) == 0;   // this lane takes the larger
             v = (low == down) == (v > w) ? v : w;
         }
@@ -552,8 +572,9 @@ __device__ __forceinline__ u64 wave_merge(u64 a, u64 b) {
     const int lane = threadIdx.x & 63;
     const u64 r = __shfl(b, 63 - lane);
     u64 v = a > r ? a : r;
+#pragma unroll
     for (int j = 32; j > 0; j >>= 1) {
-        const u64 w = __shfl_xor(v, j);
+        const u64 w = lane_xor64(v, j);
         v = ((lane & j) == 0) == (v > w) ? v : w;
     }
     return v;
@@ -579,7 +600,7 @@ __device__ void draw_few(const SampleArgs& a, const RowSettings& set, u64 best, 
         return;
     }
     const bool first = !(set.t > 0.f) || set.mp > 1.f;
-    const Weigh w{(double)key_f32((uint32_t)__shfl((int)key, 0)), (double)set.t, ldexp(1., bits)};
+    const Weigh w{(double)key_f32((uint32_t)__builtin_amdgcn_readfirstlane((int)key)), (double)set.t, ldexp(1., bits)};
     u64 x = first ? (u64)(lane == 0) << bits : lane < n ? w.weight(key) : 0ull;
     if (first) n = 1;
     u64 c = x;
@@ -588,18 +609,15 @@ __device__ void draw_few(const SampleArgs& a, const RowSettings& set, u64 best, 
         if (lane >= o) c += up;
     }
     if (set.p < 1.f && !first) {
-        const double want = ceil((double)set.p * (double)__shfl(c, 63));
+        const double want = ceil((double)set.p * (double)lane_value(c, 63));
         n = min(n, __popcll(__ballot(lane < n && (double)c < want)) + 1);
     }
     if (set.mp > 0.f && !first) n = max(1, min(n, __popcll(__ballot(lane < n && exp(w.power(key)) >= (double)set.mp))));
-    const u64 total = __shfl(c, n - 1);
+    const u64 total = lane_value(c, n - 1);
     const u64 target = (u64)(unit(a.uniform[r]) * (double)total);
     u64 before = 0;   // of the kept with a lower id
-    for (int o = 0; o < n; ++o) {
-        const int other = __shfl(id, o);
-        const u64 xo = __shfl(x, o);
-        before += other < id ? xo : 0ull;
-    }
+    for (int o = 0; o < n; ++o)
+        before += __builtin_amdgcn_readlane(id, o) < id ? lane_value(x, o) : 0ull;
     if (lane < n && before <= target && target < before + x) {
         a.token[r] = id;
         if (a.logprob != nullptr) a.logprob[r] = first ? 0.f : (float)(w.power(key) - log((double)total / w.one));
@@ -642,8 +660,8 @@ __device__ bool pick_few(const SampleArgs& a, const RowSettings& set, const Slic
     const int count = sh.count;
     if (count > kSurvivors) return false;
     if (wave == 0) {
-        u64 best = 0;
-        for (int i = 0; i < count; i += kWave) best = wave_merge(best, wave_sort(i + lane < count ? sh.list[i + lane] : 0ull));
+        u64 best = wave_sort(lane < count ? sh.list[lane] : 0ull);
+        for (int i = kWave; i < count; i += kWave) best = wave_merge(best, wave_sort(i + lane < count ? sh.list[i + lane] : 0ull));
         draw_few(a, set, best, n, bits);
     }
     return true;
@@ -656,9 +674,10 @@ struct WholeShared {
     uint32_t count[kSteps];
     double upto[kSteps];      // mass of steps 0..j, the largest logit's weight being 1
     double unit[kSteps];      // weight of a step's middle
-    u64 list[kBorderList];    // the border's step: key << 32 | ~id, ranked
+    u64 list[kBorderList];    // the border's step: key << 32 | ~id
     u64 border[kMaxSlices];   // kept mass of that step, by slice
     double slice[kMaxSlices];
+    unsigned short holds[kMaxSlices];
     int listed, cut, pick, last;
 };
 
@@ -697,77 +716,131 @@ struct Whole {
     u64* tmp;
     const T* row;
     int slices, skip, r;
-    double per, top, ytop, one;
+    double per, ytop, one;
+    int top;
     float largest;
+    Series weight;
 
-    __device__ int step_below(const SliceHead& h) const {   // steps from the row's top to the slice's
-        const double d = top - h.top;
-        return d < (double)kSteps ? (int)d : kSteps;
+    // steps from the row's top to the slice's
+    __device__ int step_below(const SliceHead& h) const {
+        return h.largest > neg_inf() ? min(top - h.top, kSteps) : kSteps;
     }
-    // Ranks the tokens of step j; false where they are too many.
-    __device__ bool rank_step(int j) {
+    // A logit's step below the top; kSteps or more: of no weight.
+    __device__ Step place(float z) const {
+        const Step s = step_of(fmaxf(z, (float)((top - (kSteps + 8)) / per)), per);
+        return {top - s.step, s.rest};
+    }
+    // Lists the tokens of step j; false where they are too many.
+    __device__ bool list_step(int j) {
         const int tid = threadIdx.x;
         constexpr int kPer = Chunk<T>::kPer;
-        if (tid == 0) sh.listed = 0;
+        if (tid == 0) sh.listed = 0, sh.pick = 0;
         __syncthreads();
-        for (int s = 0; s < slices; ++s) {
+        // the slices that hold any
+        for (int s = tid; s < slices; s += kSampleThreads) {
             const SliceHead h = data[s].head;
             const int at = j - step_below(h);
-            if (!(h.largest > neg_inf()) || at < 0 || at >= h.used || data[s].whole.mass[at] == 0) continue;   // uniform
-            const int end = min((s + 1) * kSlice, a.V + skip);
-            for (int v = s * kSlice + tid * kPer; v < end; v += kSampleThreads * kPer) {
-                const u32x4 raw = *reinterpret_cast<const u32x4*>(row - skip + v);
+            if (at >= 0 && at < h.used && data[s].whole.mass[at] != 0) sh.holds[atomicAdd(&sh.pick, 1)] = (unsigned short)s;
+        }
+        __syncthreads();
+        const int vecs = sh.pick * (kSlice / kPer);
+        // a wider range in fp32 first, which few pass
+        const float lo = (float)((top - j - 0.51) / per), hi = (float)((top - j + 0.51) / per);
+        const float under = lo - fabsf(lo) * 0x1p-22f, over = hi + fabsf(hi) * 0x1p-22f;
+        const u32x4* p = reinterpret_cast<const u32x4*>(row - skip);
+        const int end = a.V + skip;
+        constexpr int kDeep = 4;   // loads in flight a thread
+        for (int i0 = tid; i0 < vecs; i0 += kDeep * kSampleThreads) {
+            u32x4 raw[kDeep];
+            int first[kDeep];
+#pragma unroll
+            for (int d = 0; d < kDeep; ++d) {
+                const int i = i0 + d * kSampleThreads;
+                first[d] = i < vecs ? sh.holds[i / (kSlice / kPer)] * kSlice + i % (kSlice / kPer) * kPer : end;
+                raw[d] = u32x4{~0u, ~0u, ~0u, ~0u};
+                if (first[d] < end) raw[d] = p[first[d] / kPer];
+            }
+#pragma unroll
+            for (int d = 0; d < kDeep; ++d)
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) {
                     float z;
-                    if (sizeof(T) == 4) z = __uint_as_float(raw[e & 3]);
-                    else z = __uint_as_float(e & 1 ? raw[(e >> 1) & 3] & 0xffff0000u : raw[(e >> 1) & 3] << 16);
-                    if (v + e < skip || v + e >= end || !(top - step_of(z, per).step == (double)j)) continue;
+                    if (sizeof(T) == 4) z = __uint_as_float(raw[d][e & 3]);
+                    else z = __uint_as_float(e & 1 ? raw[d][(e >> 1) & 3] & 0xffff0000u : raw[d][(e >> 1) & 3] << 16);
+                    if (!(z >= under && z <= over)) continue;
+                    const int v = first[d] + e;
+                    if (v < skip || v >= end || place(z).step != j) continue;
                     const int slot = atomicAdd(&sh.listed, 1);
-                    if (slot < kBorderList) sh.list[slot] = (u64)logit_key(z) << 32 | (uint32_t)~(v + e - skip);
+                    if (slot < kBorderList) sh.list[slot] = (u64)logit_key(z) << 32 | (uint32_t)~(v - skip);
                 }
-            }
         }
         __syncthreads();
-        const int n = sh.listed;
-        if (n > kBorderList) return false;
-        int size = 2;
-        while (size < n) size <<= 1;
-        for (int i = n + tid; i < size; i += kSampleThreads) sh.list[i] = 0;
-        __syncthreads();
-        for (int k = 2; k <= size; k <<= 1)
-            for (int m = k >> 1; m > 0; m >>= 1) {
-                for (int i = tid; i < size / 2; i += kSampleThreads) {
-                    const int lo = (i / m) * 2 * m + i % m, hi = lo + m;
-                    const u64 x = sh.list[lo], y = sh.list[hi];
-                    if (((lo & k) == 0) == (x < y)) sh.list[lo] = y, sh.list[hi] = x;
-                }
-                __syncthreads();
-            }
-        return true;
+        return sh.listed <= kBorderList;
     }
-    __device__ u64 listed_weight(int i) const { return fixed_rest(step_of(key_f32((uint32_t)(sh.list[i] >> 32)), per).rest, one); }
-    // Weights of the ranked step's first `n` tokens, and how many of them it
-    // takes to reach `target` of them (n if all together do not).
-    __device__ double ranked_mass(int n, double target, int* reach) {
-        constexpr int kPer = kBorderList / kSampleThreads;
+    __device__ u64 weight_of(u64 entry) const { return weight(place(key_f32((uint32_t)(entry >> 32))).rest); }
+
+    // Entries of the listed step, a thread's share of them.
+    template <class F>
+    __device__ void each_listed(F f) const {
+        for (int i = threadIdx.x; i < sh.listed; i += kSampleThreads) f(sh.list[i]);
+    }
+    // Smallest or largest of a value a thread.
+    template <bool MAX>
+    __device__ u64 block_extreme(u64 v) {
+#pragma unroll
+        for (int j = 32; j > 0; j >>= 1) {
+            const u64 w = lane_xor64(v, j);
+            v = (v > w) == MAX ? v : w;
+        }
+        if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = tmp[0];
+        for (int w = 1; w < kSampleWaves; ++w) v = (v > tmp[w]) == MAX ? v : tmp[w];
+        __syncthreads();
+        return v;
+    }
+    // The listed entry, at least `from`, at which those from the largest down
+    // reach `target` weights (BY_MASS) or entries, found nine bits at a time
+    // among the bits in which what is left differs; the last one if all
+    // together do not.
+    template <bool BY_MASS>
+    __device__ u64 reach(double target, u64 from) {
         const int tid = threadIdx.x;
-        u64 x[kPer], sum = 0;
-        for (int e = 0; e < kPer; ++e) {
-            const int i = tid * kPer + e;
-            x[e] = i < n ? listed_weight(i) : 0ull;
-            sum += x[e];
+        u64 lo = from, hi = ~0ull, above = 0;
+        for (;;) {
+            u64 mn = ~0ull, mx = 0;
+            each_listed([&](u64 x) {
+                if (x < lo || x > hi) return;
+                mn = x < mn ? x : mn;
+                mx = x > mx ? x : mx;
+            });
+            mn = block_extreme<false>(mn);
+            mx = block_extreme<true>(mx);
+            if (mn >= mx) return mn;   // entries differ: one is left
+            const int bits = 64 - __builtin_clzll(mn ^ mx), shift = bits > 9 ? bits - 9 : 0;
+            sh.mass[tid] = 0;
+            __syncthreads();
+            each_listed([&](u64 x) {
+                if (x >= lo && x <= hi) atomicAdd(&sh.mass[kSteps - 1 - (int)((x >> shift) & (kSteps - 1))], BY_MASS ? weight_of(x) : 1ull);
+            });
+            __syncthreads();
+            const u64 here = sh.mass[tid], upto = above + block_before(here, tmp);
+            const int bin = block_min((double)(upto + here) >= target ? tid : 0x7fffffff, &sh.cut);
+            if (bin == 0x7fffffff) return mn;
+            if (tid == bin) tmp[0] = upto;
+            __syncthreads();
+            above = tmp[0];
+            __syncthreads();
+            lo = (mn >> shift & ~(u64)(kSteps - 1) | (u64)(kSteps - 1 - bin)) << shift;
+            hi = lo | ((1ull << shift) - 1);
+            if (shift == 0) return lo;
         }
-        u64 at = block_before(sum, tmp);
-        const u64 all = block_sum(sum);
-        int found = 0x7fffffff;
-        for (int e = 0; e < kPer; ++e) {
-            at += x[e];
-            if (found == 0x7fffffff && tid * kPer + e < n && (double)at >= target) found = tid * kPer + e;
-        }
-        found = block_min(found, &sh.cut);
-        if (reach != nullptr) *reach = found < n ? found + 1 : n;
-        return (double)all;
+    }
+    // Weights of the listed entries from `from` up.
+    __device__ double mass_from(u64 from) {
+        u64 sum = 0;
+        each_listed([&](u64 x) { sum += x >= from ? weight_of(x) : 0ull; });
+        return (double)block_sum(sum);
     }
     __device__ u64 block_sum(u64 v) {
         const u64 before = block_before(v, tmp);
@@ -790,7 +863,7 @@ struct Whole {
         const bool counted = set.k > 0;
         for (int s = wave; s < slices; s += kSampleWaves) {
             const SliceHead h = data[s].head;
-            const int below = h.largest > neg_inf() ? step_below(h) : kSteps;
+            const int below = step_below(h);
             for (int j = lane; j < h.used && j + below < kSteps; j += kWave) {
                 const u64 m = data[s].whole.mass[j];
                 if (m != 0) atomicAdd(&sh.mass[j + below], m);
@@ -798,72 +871,69 @@ struct Whole {
             }
         }
         __syncthreads();
-        // thread j < kSteps is step j
-        const double weight = tid < kSteps ? exp(((top - ytop) - (double)tid) * 0.125) / one : 0.;
-        const double upto = block_upto(tid < kSteps ? (double)sh.mass[tid] * weight : 0., reinterpret_cast<double*>(tmp));
-        if (tid < kSteps) sh.unit[tid] = weight, sh.upto[tid] = upto;
+        // thread j is step j
+        static_assert(kSteps == kSampleThreads, "a step a thread");
+        const double each = exp((((double)top - ytop) - (double)tid) * 0.125) / one;
+        sh.upto[tid] = block_upto((double)sh.mass[tid] * each, reinterpret_cast<double*>(tmp));
+        sh.unit[tid] = each;
         __syncthreads();
-        // the kept: steps above `edge` whole, of that one the first `part` ranked tokens
-        int edge = kSteps, part = 0, ranked = -1;
+        // the kept: steps above `edge` whole, of that one the entries from `least` up
+        int edge = kSteps, listed = -1;
+        u64 least = 0;
         double total = sh.upto[kSteps - 1];
+        auto above = [&](int j) { return j > 0 ? sh.upto[j - 1] : 0.; };
         if (counted && set.k < a.V) {
-            const u64 n = block_before(tid < kSteps ? sh.count[tid] : 0u, tmp);
-            const int j = block_min(tid < kSteps && n + sh.count[tid] >= (u64)set.k ? tid : 0x7fffffff, &sh.cut);
+            const u64 n = block_before(sh.count[tid], tmp);
+            const int j = block_min(n + sh.count[tid] >= (u64)set.k ? tid : 0x7fffffff, &sh.cut);
             if (j < kSteps) {
-                if (tid == j) sh.cut = set.k - (int)n;
+                if (tid == j) tmp[0] = set.k - n;
                 __syncthreads();
-                part = sh.cut;
+                const double more = (double)tmp[0];
                 __syncthreads();
-                if (!rank_step(j)) return false;
-                edge = ranked = j;
-                total = (j > 0 ? sh.upto[j - 1] : 0.) + ranked_mass(part, 0., nullptr) * sh.unit[j];
+                if (!list_step(j)) return false;
+                edge = listed = j;
+                least = reach<false>(more, 0);
+                total = above(j) + mass_from(least) * sh.unit[j];
             }
         }
         if (set.p < 1.f) {
             const double target = (double)set.p * total;
-            int j = block_min(tid < min(edge + 1, kSteps) && sh.upto[min(tid, kSteps - 1)] >= target ? tid : 0x7fffffff, &sh.cut);
+            int j = block_min(tid <= edge && sh.upto[tid] >= target ? tid : 0x7fffffff, &sh.cut);
             if (j == 0x7fffffff && edge < kSteps) j = edge;   // the border's own rounding
             if (j < kSteps) {
-                const double above = j > 0 ? sh.upto[j - 1] : 0.;
-                if (j != ranked) {
-                    if (!rank_step(j)) return false;
-                    ranked = j;
-                    part = sh.listed;
-                }
-                edge = j;
-                const int most = part;
-                ranked_mass(most, (target - above) / sh.unit[j], &part);
-                total = above + ranked_mass(part, 0., nullptr) * sh.unit[j];
+                if (j != listed && !list_step(j)) return false;
+                if (j != edge) least = 0;
+                edge = listed = j;
+                least = reach<true>((target - above(j)) / sh.unit[j], least);
+                total = above(j) + mass_from(least) * sh.unit[j];
             }
         }
         if (set.mp > 0.f) {
-            const double least = (double)set.mp;
-            const double d = top - rint(ytop + 8. * log(least));
+            const double floor = (double)set.mp;
+            const double d = (double)top - rint(ytop + 8. * log(floor));
             const int j = d < (double)kSteps ? (int)d : kSteps;
             if (j <= edge && j < kSteps) {
-                if (j != ranked) {
-                    if (!rank_step(j)) return false;
-                    ranked = j;
-                    part = sh.listed;
-                }
-                edge = j;
-                int n = 0;
-                for (int i = tid; i < part; i += kSampleThreads) {
-                    const double x = ((double)key_f32((uint32_t)(sh.list[i] >> 32)) - (double)largest) / (double)set.t;
-                    n += exp(x) >= least ? 1 : 0;
-                }
-                part = (int)block_sum((u64)n);
-                total = (j > 0 ? sh.upto[j - 1] : 0.) + ranked_mass(part, 0., nullptr) * sh.unit[j];
+                if (j != listed && !list_step(j)) return false;
+                if (j != edge) least = 0;
+                edge = listed = j;
+                u64 first = ~0ull;   // none: the steps above alone
+                each_listed([&](u64 x) {
+                    const double z = ((double)key_f32((uint32_t)(x >> 32)) - (double)largest) / (double)set.t;
+                    if (x >= least && x < first && exp(z) >= floor) first = x;
+                });
+                least = block_extreme<false>(first);
+                total = above(j) + mass_from(least) * sh.unit[j];
             }
         }
-        const u64 least = part > 0 ? sh.list[part - 1] : ~0ull;   // of the edge's step, what ranks no later
-        for (int i = tid; i < part; i += kSampleThreads)
-            atomicAdd(&sh.border[((int)~(uint32_t)sh.list[i] + skip) / kSlice], listed_weight(i));
+        if (edge < kSteps)
+            each_listed([&](u64 x) {
+                if (x >= least) atomicAdd(&sh.border[((int)~(uint32_t)x + skip) / kSlice], weight_of(x));
+            });
         if (tid == 0) sh.pick = 0x7fffffff, sh.last = -1;
         __syncthreads();
         for (int s = wave; s < slices; s += kSampleWaves) {
             const SliceHead h = data[s].head;
-            const int below = h.largest > neg_inf() ? step_below(h) : kSteps;
+            const int below = step_below(h);
             double m = 0.;
             for (int j = lane; j < h.used && j + below < edge; j += kWave) m += (double)data[s].whole.mass[j] * sh.unit[j + below];
             for (int o = 32; o > 0; o >>= 1) m += __shfl_xor(m, o);
@@ -886,29 +956,29 @@ struct Whole {
             if (m > 0. && sum > target) break;
         }
         constexpr int kEach = kSlice / kSampleThreads;
+        const int v0 = at * kSlice + tid * kEach;
         double w[kEach], mine = 0.;
+#pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const int v = at * kSlice + tid * kEach + e;
-            w[e] = 0.;
-            if (v < skip || v >= a.V + skip) continue;
-            const uint32_t key = key_at(row, v - skip);
-            if (key <= kKeyNone) continue;
-            const Step st = step_of(key_f32(key), per);
-            const double d = top - st.step;
-            if (!(d < (double)kSteps) || (int)d > edge) continue;
-            if ((int)d == edge && ((u64)key << 32 | (uint32_t)~(v - skip)) < least) continue;
-            w[e] = (double)fixed_rest(st.rest, one) * sh.unit[(int)d];
+            const int v = v0 + e;
+            const uint32_t key = v >= skip && v < a.V + skip ? key_at(row, v - skip) : 0u;
+            const Step st = place(key_f32(max(key, kKeyNone)));   // no token: beyond the steps
+            const bool kept = st.step < kSteps && (st.step < edge || (st.step == edge && ((u64)key << 32 | (uint32_t)~(v - skip)) >= least));
+            w[e] = kept ? (double)weight(st.rest) * sh.unit[min(st.step, kSteps - 1)] : 0.;
             mine += w[e];
         }
         double run = before + block_upto(mine, reinterpret_cast<double*>(tmp)) - mine;
+        int pick = 0x7fffffff, last = -1;
+#pragma unroll
+        for (int e = kEach - 1; e >= 0; --e)
+            if (w[e] > 0.) last = max(last, v0 + e);
+#pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const int v = at * kSlice + tid * kEach + e;
             run += w[e];
-            if (w[e] > 0.) {
-                atomicMax(&sh.last, v);
-                if (run > target) atomicMin(&sh.pick, v);
-            }
+            if (w[e] > 0. && run > target) pick = min(pick, v0 + e);
         }
+        if (pick != 0x7fffffff) atomicMin(&sh.pick, pick);
+        if (last >= 0) atomicMax(&sh.last, last);
         __syncthreads();
         if (tid == 0) {
             const int v = (sh.pick != 0x7fffffff ? sh.pick : sh.last) - skip;
@@ -922,7 +992,7 @@ struct Whole {
 
 // A workgroup a row.
 template <class T>
-__global__ __launch_bounds__(kSampleThreads) void pick_kernel(SampleArgs a, int slices, int bits) {
+__global__ __launch_bounds__(kSampleThreads, 4) void pick_kernel(SampleArgs a, int slices, int bits) {
     __shared__ union {
         FewShared few;
         WholeShared whole;
@@ -951,11 +1021,12 @@ __global__ __launch_bounds__(kSampleThreads) void pick_kernel(SampleArgs a, int 
             }
             return;
         }
-        if (largest < __builtin_inff()) {
+        const double per = 8. / (double)set.t, ytop = (double)largest * per;
+        if (fabs(ytop) < kFar) {
             const T* row = static_cast<const T*>(a.logits) + (size_t)r * a.ld;
-            const double per = 8. / (double)set.t;
-            Whole<T> w{a, set, data, sh.whole, tmp, row, slices, Chunk<T>::skip_of(row), r, per,
-                       step_of(largest, per).step, steps_at(largest, per), ldexp(1., bits), largest};
+            const double one = ldexp(1., bits);
+            Whole<T> w{a, set, data, sh.whole, tmp, row, slices, Chunk<T>::skip_of(row), r, per, ytop, one,
+                       step_of(largest, per).step, largest, Series(one)};
             if (w.draw()) return;
         }
     }
