@@ -13,7 +13,7 @@
 //   few   (top-k of at most 64, or the largest alone) -- of each 2048 logits
 //         the ones that can be among the row's best k;
 //   whole (else) -- masses of the slice by the value's distance from its
-//         largest, in steps of 1/8.
+//         largest, in steps of 1/16.
 // pick_kernel joins a row's slices.  `few` rows are ranked in one wave.  For
 // `whole` rows the steps' masses give each filter's border to one step; the
 // tokens of that step alone are looked up again and ranked, and once the
@@ -28,15 +28,17 @@ namespace tf {
 
 constexpr int kSampleThreads = 512;
 constexpr int kSampleWaves = kSampleThreads / kWave;
-constexpr int kSampleTile = 4 * kSampleThreads;   // ids of the draw's first step
+constexpr int kSampleTile = 4096;   // ids of the draw's first step
+constexpr int kTileEach = kSampleTile / kSampleThreads;
 constexpr int kSlice = 8192;                      // logits a workgroup of the scan reads
 constexpr int kScanThreads = 256;
 constexpr int kScanWaves = kScanThreads / kWave;
 constexpr int kChunk = kSlice / kScanWaves;       // of a wave
 constexpr int kFew = 64;                          // tokens that one wave ranks
 constexpr int kList = 128;                        // of a chunk, entries kept
-constexpr int kSteps = 512;                       // of 1/8 below a slice's largest: e^-64 is nothing
-constexpr int kSurvivors = 2048, kBorderList = 4096;
+constexpr int kSteps = 512;                       // of 1/16: e^-32 of the largest is no weight (2^-46)
+constexpr int kPerUnit = 16;
+constexpr int kSurvivors = 2048, kBorderList = 2048;
 constexpr uint32_t kKeyNone = 0x007fffffu;        // -inf's key: that and below is no token
 typedef unsigned long long u64;
 
@@ -251,21 +253,24 @@ __device__ __noinline__ void hard_row(const SampleArgs& a, const RowSettings& se
     }
     __syncthreads();
     const u64 target = s_state[1], left = s_state[2], total = s_state[3];
-    const int i0 = (int)s_state[0] * kSampleTile + tid * 4;
-    uint32_t key[4];
-    u64 x[4], ties = 0, sum = 0;
-    for (int j = 0; j < 4; ++j) {
+    const int i0 = (int)s_state[0] * kSampleTile + tid * kTileEach;
+    uint32_t key[kTileEach];
+    u64 x[kTileEach], ties = 0, sum = 0;
+#pragma unroll
+    for (int j = 0; j < kTileEach; ++j) {
         key[j] = i0 + j < V ? key_at(row, i0 + j) : 0u;
         x[j] = weight(key[j]);
         ties += x[j] == 0 && !whole && key[j] == kept.key && key[j] > kKeyNone && tie_ok ? 1 : 0;
     }
     u64 tie_at = block_before(ties, tmp);
-    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int j = 0; j < kTileEach; ++j) {
         if (x[j] == 0 && !whole && key[j] == kept.key && key[j] > kKeyNone && tie_ok && tie_at++ < left) x[j] = tie_w;
         sum += x[j];
     }
     u64 at = block_before(sum, tmp);
-    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int j = 0; j < kTileEach; ++j) {
         if (at <= target && target < at + x[j]) {
             a.token[r] = i0 + j;
             if (a.logprob != nullptr) a.logprob[r] = (float)(w.power(key[j]) - log((double)total / w.one));
@@ -294,10 +299,17 @@ struct SliceData {
         struct {
             u64 mass[kSteps];
             uint32_t count[kSteps];
-        } whole;
+        };
         ChunkList few[kScanWaves];
     };
 };
+
+// Logit e of a 16-byte vector.
+template <class T>
+__device__ __forceinline__ float vector_at(const u32x4& x, int e) {
+    if (sizeof(T) == 4) return __uint_as_float(x[e & 3]);
+    return __uint_as_float(e & 1 ? x[(e >> 1) & 3] & 0xffff0000u : x[(e >> 1) & 3] << 16);
+}
 
 // Vectors of 16 bytes that a lane holds of a chunk; the row is read from the
 // 16-byte boundary at or before its first logit, `skip` logits earlier.
@@ -329,11 +341,7 @@ struct Chunk {
                 else raw[i][(e >> 1) & 3] |= e & 1 ? 0xffff0000u : 0xffffu;
             }
     }
-    __device__ float at(int i, int e) const {
-        if (sizeof(T) == 4) return __uint_as_float(raw[i][e & 3]);
-        const uint32_t w = raw[i][(e >> 1) & 3];
-        return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
-    }
+    __device__ float at(int i, int e) const { return vector_at<T>(raw[i], e); }
 };
 
 __device__ __forceinline__ int lanes_below(unsigned long long m) {
@@ -434,8 +442,8 @@ __device__ void scan_few(const Chunk<T>& c, int first, int skip, int n, ChunkLis
     }
 }
 
-// Where a logit lies: y = 8 z / T, its step b (the nearest integer) and exp of
-// what is left, |rest| <= 1/16, by its series to the 7th power (error 2^-47).
+// Where a logit lies: y = 16 z / T, its step b (the nearest integer) and exp
+// of what is left, |rest| <= 1/32, by its series to the 6th power (error 2^-47).
 // Adding 1.5 * 2^52 rounds to an integer and leaves it in the sum's low bits,
 // which takes three operations for step and rest.  Rows whose largest |y| is
 // 2^20 or more (kFar) are left to hard_row: there a step is no longer far
@@ -450,23 +458,24 @@ __device__ __forceinline__ Step step_of(float z, double per) {
     const double t = fma((double)z, per, kRound), b = t - kRound;
     return {(int)(uint32_t)__double_as_longlong(t), fma((double)z, per, -b)};
 }
-// exp(rest / 8) as an integer, 2^bits the one (bits <= 48): the coefficients
+// exp(rest / 16) as an integer, 2^bits the one (bits <= 48): the coefficients
 // carry that factor, and a constant term 2^52 more rounds the sum and leaves
 // the integer in its low bits.
 struct Series {
-    double c[8];
+    double c[7];
     __device__ explicit Series(double one) {
         double f = one;
-        for (int n = 0; n < 8; ++n) {
+#pragma unroll
+        for (int n = 0; n < 7; ++n) {
             c[n] = f;
-            f *= 0.125 / (n + 1);
+            f *= 1. / kPerUnit / (n + 1);
         }
         c[0] += 0x1p52;
     }
     __device__ u64 operator()(double r) const {
-        double s = c[7];
+        double s = c[6];
 #pragma unroll
-        for (int n = 6; n >= 0; --n) s = fma(s, r, c[n]);
+        for (int n = 5; n >= 0; --n) s = fma(s, r, c[n]);
         return (u64)__double_as_longlong(s) & ((1ull << 52) - 1);
     }
 };
@@ -495,7 +504,7 @@ __device__ void scan_whole(const Chunk<T>& c, const RowSettings& set, double one
     if (lane == 0) sh.top[wave] = mx;
     __syncthreads();
     for (int w = 0; w < kScanWaves; ++w) mx = fmaxf(mx, sh.top[w]);
-    const double per = 8. / (double)set.t;
+    const double per = kPerUnit / (double)set.t;
     const bool counted = set.k > 0;
     int last = -1, top = 0;
     if (mx > neg_inf() && fabs((double)mx * per) < kFar) {
@@ -520,8 +529,8 @@ __device__ void scan_whole(const Chunk<T>& c, const RowSettings& set, double one
     __syncthreads();
     const int used = sh.used;
     for (int j = tid; j < used; j += kScanThreads) {
-        out->whole.mass[j] = sh.mass[j];
-        if (counted) out->whole.count[j] = sh.count[j];
+        out->mass[j] = sh.mass[j];
+        if (counted) out->count[j] = sh.count[j];
     }
     if (tid == 0) out->head = {top, used, mx, 0};
 }
@@ -540,8 +549,11 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(SampleArgs a, int bi
     Chunk<T> c;
     c.load(row, skip, a.V, first);
     const int n = set.few(a.V);
-    if (n > 0) scan_few(c, first, skip, n, &out->few[wave]);
-    else scan_whole(c, set, ldexp(1., bits), sh, out);
+    if (n > 0) {
+        scan_few(c, first, skip, n, &out->few[wave]);
+    } else {
+        scan_whole(c, set, ldexp(1., bits), sh, out);
+    }
 }
 
 // ------------------------------------------------------------------ the pick
@@ -578,6 +590,32 @@ __device__ __forceinline__ u64 wave_merge(u64 a, u64 b) {
         v = ((lane & j) == 0) == (v > w) ? v : w;
     }
     return v;
+}
+
+// A row's list entries, dealt out over the workgroup: a wave a list, with the
+// loads of several lists in flight (what lies behind a list's end is read, but
+// not used).
+template <class F>
+__device__ __forceinline__ void each_entry(const SliceData* data, int lists, F f) {
+    constexpr int kDeep = 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int i0 = wave; i0 < lists; i0 += kDeep * kSampleWaves) {
+        u64 x[kDeep][kList / kWave];
+        int count[kDeep];
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+            const int i = min(i0 + d * kSampleWaves, lists - 1);
+            const ChunkList& l = data[i / kScanWaves].few[i % kScanWaves];
+            count[d] = i0 + d * kSampleWaves < lists ? l.count : 0;
+#pragma unroll
+            for (int h = 0; h < kList / kWave; ++h) x[d][h] = l.entry[h * kWave + lane];
+        }
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d)
+#pragma unroll
+            for (int h = 0; h < kList / kWave; ++h)
+                if (h * kWave + lane < count[d]) f(x[d][h]);
+    }
 }
 
 struct FewShared {
@@ -633,10 +671,7 @@ __device__ bool pick_few(const SampleArgs& a, const RowSettings& set, const Slic
     const int lists = slices * kScanWaves;
     if (n == 1) {
         u64 best = 0;
-        for (int i = wave; i < lists; i += kSampleWaves) {
-            const ChunkList& l = data[i / kScanWaves].few[i % kScanWaves];
-            for (int e = lane; e < l.count; e += kWave) best = l.entry[e] > best ? l.entry[e] : best;
-        }
+        each_entry(data, lists, [&](u64 x) { best = x > best ? x : best; });
         best = block_max(best, tmp);
         if (wave == 0) draw_few(a, set, lane == 0 ? best : 0ull, 1, bits);
         return true;
@@ -646,16 +681,11 @@ __device__ bool pick_few(const SampleArgs& a, const RowSettings& set, const Slic
     const uint32_t bound = reached_by(logit_key(mx), n);
     if (tid == 0) sh.count = 0;
     __syncthreads();
-    for (int i = wave; i < lists; i += kSampleWaves) {
-        const ChunkList& l = data[i / kScanWaves].few[i % kScanWaves];
-        const int count = l.count;
-        for (int e = lane; e < count; e += kWave) {
-            const u64 x = l.entry[e];
-            if ((uint32_t)(x >> 32) < bound) continue;
-            const int at = atomicAdd(&sh.count, 1);
-            if (at < kSurvivors) sh.list[at] = x;
-        }
-    }
+    each_entry(data, lists, [&](u64 x) {
+        if ((uint32_t)(x >> 32) < bound) return;
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < kSurvivors) sh.list[at] = x;
+    });
     __syncthreads();
     const int count = sh.count;
     if (count > kSurvivors) return false;
@@ -675,6 +705,7 @@ struct WholeShared {
     double upto[kSteps];      // mass of steps 0..j, the largest logit's weight being 1
     double unit[kSteps];      // weight of a step's middle
     u64 list[kBorderList];    // the border's step: key << 32 | ~id
+    u64 ends[2][kSampleWaves];
     u64 border[kMaxSlices];   // kept mass of that step, by slice
     double slice[kMaxSlices];
     unsigned short holds[kMaxSlices];
@@ -730,6 +761,21 @@ struct Whole {
         const Step s = step_of(fmaxf(z, (float)((top - (kSteps + 8)) / per)), per);
         return {top - s.step, s.rest};
     }
+    // The lowest (UP false) or highest logit of step j.
+    template <bool UP>
+    __device__ float step_end(int j) const {
+        const double edge = UP ? (top - j + 0.5) / per : (top - j - 0.5) / per;
+        const float z = (float)edge;
+        // the nearest fp32 values around the edge, the outermost that is in the step
+        const uint32_t key = f32_key(z);
+        float found = key_f32(key);
+#pragma unroll 1
+        for (int d = 2; d >= -2; --d) {
+            const float c = key_f32(UP ? key - d : key + d);   // from inside the step outwards
+            if (place(c).step == j) found = c;
+        }
+        return found;
+    }
     // Lists the tokens of step j; false where they are too many.
     __device__ bool list_step(int j) {
         const int tid = threadIdx.x;
@@ -740,16 +786,14 @@ struct Whole {
         for (int s = tid; s < slices; s += kSampleThreads) {
             const SliceHead h = data[s].head;
             const int at = j - step_below(h);
-            if (at >= 0 && at < h.used && data[s].whole.mass[at] != 0) sh.holds[atomicAdd(&sh.pick, 1)] = (unsigned short)s;
+            if (at >= 0 && at < h.used && data[s].mass[at] != 0) sh.holds[atomicAdd(&sh.pick, 1)] = (unsigned short)s;
         }
         __syncthreads();
-        const int vecs = sh.pick * (kSlice / kPer);
-        // a wider range in fp32 first, which few pass
-        const float lo = (float)((top - j - 0.51) / per), hi = (float)((top - j + 0.51) / per);
-        const float under = lo - fabsf(lo) * 0x1p-22f, over = hi + fabsf(hi) * 0x1p-22f;
+        // a step is a range of logits: its ends, exactly
+        const float lo = step_end<false>(j), hi = step_end<true>(j);
         const u32x4* p = reinterpret_cast<const u32x4*>(row - skip);
-        const int end = a.V + skip;
-        constexpr int kDeep = 4;   // loads in flight a thread
+        const int vecs = sh.pick * (kSlice / kPer), end = a.V + skip;
+        constexpr int kDeep = 32 / kPer;   // loads in flight a thread, 32 logits
         for (int i0 = tid; i0 < vecs; i0 += kDeep * kSampleThreads) {
             u32x4 raw[kDeep];
             int first[kDeep];
@@ -760,19 +804,39 @@ struct Whole {
                 raw[d] = u32x4{~0u, ~0u, ~0u, ~0u};
                 if (first[d] < end) raw[d] = p[first[d] / kPer];
             }
+            uint32_t hit = 0;   // of the lane's logits
 #pragma unroll
             for (int d = 0; d < kDeep; ++d)
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) {
-                    float z;
-                    if (sizeof(T) == 4) z = __uint_as_float(raw[d][e & 3]);
-                    else z = __uint_as_float(e & 1 ? raw[d][(e >> 1) & 3] & 0xffff0000u : raw[d][(e >> 1) & 3] << 16);
-                    if (!(z >= under && z <= over)) continue;
-                    const int v = first[d] + e;
-                    if (v < skip || v >= end || place(z).step != j) continue;
-                    const int slot = atomicAdd(&sh.listed, 1);
-                    if (slot < kBorderList) sh.list[slot] = (u64)logit_key(z) << 32 | (uint32_t)~(v - skip);
+                    const float z = vector_at<T>(raw[d], e);
+                    hit |= z >= lo && z <= hi ? 1u << (d * kPer + e) : 0u;
                 }
+#pragma unroll
+            for (int d = 0; d < kDeep; ++d)   // at the row's ends, what is no logit of it
+                if (first[d] < skip || first[d] + kPer > end)
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e)
+                        if (first[d] + e < skip || first[d] + e >= end) hit &= ~(1u << (d * kPer + e));
+            if (__any(hit != 0)) {
+                int at = __popc(hit);
+                for (int o = 1; o < kWave; o <<= 1) {
+                    const int up = __shfl_up(at, o);
+                    if ((tid & 63) >= o) at += up;
+                }
+                int base = 0;
+                if ((tid & 63) == 63) base = atomicAdd(&sh.listed, at);
+                at += __builtin_amdgcn_readlane(base, 63) - __popc(hit);
+#pragma unroll
+                for (int d = 0; d < kDeep; ++d)
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e)
+                        if (hit >> (d * kPer + e) & 1) {
+                            if (at < kBorderList)
+                                sh.list[at] = (u64)logit_key(vector_at<T>(raw[d], e)) << 32 | (uint32_t)~(first[d] + e - skip);
+                            ++at;
+                        }
+            }
         }
         __syncthreads();
         return sh.listed <= kBorderList;
@@ -784,20 +848,46 @@ struct Whole {
     __device__ void each_listed(F f) const {
         for (int i = threadIdx.x; i < sh.listed; i += kSampleThreads) f(sh.list[i]);
     }
-    // Smallest or largest of a value a thread.
-    template <bool MAX>
-    __device__ u64 block_extreme(u64 v) {
+    // Smallest and largest of a value a thread.
+    __device__ void block_extremes(u64& mn, u64& mx) {
 #pragma unroll
         for (int j = 32; j > 0; j >>= 1) {
-            const u64 w = lane_xor64(v, j);
-            v = (v > w) == MAX ? v : w;
+            const u64 a = lane_xor64(mn, j), b = lane_xor64(mx, j);
+            mn = a < mn ? a : mn;
+            mx = b > mx ? b : mx;
         }
-        if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
+        if ((threadIdx.x & 63) == 0) sh.ends[0][threadIdx.x >> 6] = mn, sh.ends[1][threadIdx.x >> 6] = mx;
         __syncthreads();
-        v = tmp[0];
-        for (int w = 1; w < kSampleWaves; ++w) v = (v > tmp[w]) == MAX ? v : tmp[w];
+        for (int w = 0; w < kSampleWaves; ++w) {
+            mn = sh.ends[0][w] < mn ? sh.ends[0][w] : mn;
+            mx = sh.ends[1][w] > mx ? sh.ends[1][w] : mx;
+        }
         __syncthreads();
-        return v;
+    }
+    // The first of kSteps values whose running sum, on top of `from`, reaches
+    // `target`, and the sum before it; 0x7fffffff: none.
+    template <class N>
+    __device__ int first_reaching(const N* v, u64 from, double target, u64* before) {
+        constexpr int kEach = kSteps / kSampleThreads;
+        const int j0 = threadIdx.x * kEach;
+        u64 sum = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) sum += v[j0 + i];
+        u64 at = from + block_before(sum, tmp);
+        int found = 0x7fffffff;
+        u64 found_at = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const u64 next = at + v[j0 + i];
+            if (found == 0x7fffffff && (double)next >= target) found = j0 + i, found_at = at;
+            at = next;
+        }
+        const int first = block_min(found, &sh.cut);
+        if (first != 0x7fffffff && found == first) tmp[0] = found_at;
+        __syncthreads();
+        *before = tmp[0];
+        __syncthreads();
+        return first;
     }
     // The listed entry, at least `from`, at which those from the largest down
     // reach `target` weights (BY_MASS) or entries, found nine bits at a time
@@ -814,23 +904,19 @@ struct Whole {
                 mn = x < mn ? x : mn;
                 mx = x > mx ? x : mx;
             });
-            mn = block_extreme<false>(mn);
-            mx = block_extreme<true>(mx);
+            block_extremes(mn, mx);
             if (mn >= mx) return mn;   // entries differ: one is left
             const int bits = 64 - __builtin_clzll(mn ^ mx), shift = bits > 9 ? bits - 9 : 0;
-            sh.mass[tid] = 0;
+            for (int j = tid; j < kSteps; j += kSampleThreads) sh.mass[j] = 0;
             __syncthreads();
             each_listed([&](u64 x) {
                 if (x >= lo && x <= hi) atomicAdd(&sh.mass[kSteps - 1 - (int)((x >> shift) & (kSteps - 1))], BY_MASS ? weight_of(x) : 1ull);
             });
             __syncthreads();
-            const u64 here = sh.mass[tid], upto = above + block_before(here, tmp);
-            const int bin = block_min((double)(upto + here) >= target ? tid : 0x7fffffff, &sh.cut);
+            u64 bin_above;
+            const int bin = first_reaching(sh.mass, above, target, &bin_above);
             if (bin == 0x7fffffff) return mn;
-            if (tid == bin) tmp[0] = upto;
-            __syncthreads();
-            above = tmp[0];
-            __syncthreads();
+            above = bin_above;
             lo = (mn >> shift & ~(u64)(kSteps - 1) | (u64)(kSteps - 1 - bin)) << shift;
             hi = lo | ((1ull << shift) - 1);
             if (shift == 0) return lo;
@@ -851,6 +937,30 @@ struct Whole {
         return all;
     }
 
+    // Every slice's steps, a slice a wave and a step a lane, all loads of a
+    // slice in flight at once (steps that it does not use hold anything); then
+    // `done`.
+    template <class F, class G>
+    __device__ void for_slices(F f, G done) const {
+        constexpr int kLoads = kSteps / kWave;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const bool counted = set.k > 0;
+        for (int s = wave; s < slices; s += kSampleWaves) {
+            const SliceHead h = data[s].head;
+            u64 m[kLoads];
+            uint32_t n[kLoads] = {};
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) m[i] = data[s].mass[i * kWave + lane];
+            if (counted)
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) n[i] = data[s].count[i * kWave + lane];
+            const int below = step_below(h);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) f(s, h, below, i * kWave + lane, m[i], n[i]);
+            done(s);
+        }
+    }
+
     // Draws the row's token; false where the row is to be read byte by byte.
     __device__ bool draw() {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -861,21 +971,26 @@ struct Whole {
         for (int s = tid; s < slices; s += kSampleThreads) sh.border[s] = 0;
         __syncthreads();
         const bool counted = set.k > 0;
-        for (int s = wave; s < slices; s += kSampleWaves) {
-            const SliceHead h = data[s].head;
-            const int below = step_below(h);
-            for (int j = lane; j < h.used && j + below < kSteps; j += kWave) {
-                const u64 m = data[s].whole.mass[j];
-                if (m != 0) atomicAdd(&sh.mass[j + below], m);
-                if (counted && m != 0) atomicAdd(&sh.count[j + below], data[s].whole.count[j]);
-            }
-        }
+        for_slices([&](int s, const SliceHead& h, int below, int j, u64 m, uint32_t n) {
+            if (j >= min(h.used, kSteps - below)) return;
+            if (m != 0) atomicAdd(&sh.mass[j + below], m);
+            if (counted && n != 0) atomicAdd(&sh.count[j + below], n);
+        }, [](int) {});
         __syncthreads();
-        // thread j is step j
-        static_assert(kSteps == kSampleThreads, "a step a thread");
-        const double each = exp((((double)top - ytop) - (double)tid) * 0.125) / one;
-        sh.upto[tid] = block_upto((double)sh.mass[tid] * each, reinterpret_cast<double*>(tmp));
-        sh.unit[tid] = each;
+        constexpr int kStepsEach = kSteps / kSampleThreads;   // a thread's, side by side
+        const int j0 = tid * kStepsEach;
+        double m[kStepsEach], sum = 0.;
+        double each = exp((((double)top - ytop) - (double)j0) * (1. / kPerUnit)) / one;
+#pragma unroll
+        for (int i = 0; i < kStepsEach; ++i) {
+            sh.unit[j0 + i] = each;
+            sum += (double)sh.mass[j0 + i] * each;
+            m[i] = sum;
+            each *= 0.93941306281347581;   // exp(-1/16)
+        }
+        const double before_mine = block_upto(sum, reinterpret_cast<double*>(tmp)) - sum;
+#pragma unroll
+        for (int i = 0; i < kStepsEach; ++i) sh.upto[j0 + i] = before_mine + m[i];
         __syncthreads();
         // the kept: steps above `edge` whole, of that one the entries from `least` up
         int edge = kSteps, listed = -1;
@@ -883,22 +998,22 @@ struct Whole {
         double total = sh.upto[kSteps - 1];
         auto above = [&](int j) { return j > 0 ? sh.upto[j - 1] : 0.; };
         if (counted && set.k < a.V) {
-            const u64 n = block_before(sh.count[tid], tmp);
-            const int j = block_min(n + sh.count[tid] >= (u64)set.k ? tid : 0x7fffffff, &sh.cut);
+            u64 n;
+            const int j = first_reaching(sh.count, 0, (double)set.k, &n);
             if (j < kSteps) {
-                if (tid == j) tmp[0] = set.k - n;
-                __syncthreads();
-                const double more = (double)tmp[0];
-                __syncthreads();
                 if (!list_step(j)) return false;
                 edge = listed = j;
-                least = reach<false>(more, 0);
+                least = reach<false>((double)(set.k - (int)n), 0);
                 total = above(j) + mass_from(least) * sh.unit[j];
             }
         }
         if (set.p < 1.f) {
             const double target = (double)set.p * total;
-            int j = block_min(tid <= edge && sh.upto[tid] >= target ? tid : 0x7fffffff, &sh.cut);
+            int j = 0x7fffffff;
+#pragma unroll
+            for (int i = kStepsEach - 1; i >= 0; --i)
+                if (j0 + i <= edge && sh.upto[j0 + i] >= target) j = j0 + i;
+            j = block_min(j, &sh.cut);
             if (j == 0x7fffffff && edge < kSteps) j = edge;   // the border's own rounding
             if (j < kSteps) {
                 if (j != listed && !list_step(j)) return false;
@@ -910,7 +1025,7 @@ struct Whole {
         }
         if (set.mp > 0.f) {
             const double floor = (double)set.mp;
-            const double d = (double)top - rint(ytop + 8. * log(floor));
+            const double d = (double)top - rint(ytop + kPerUnit * log(floor));
             const int j = d < (double)kSteps ? (int)d : kSteps;
             if (j <= edge && j < kSteps) {
                 if (j != listed && !list_step(j)) return false;
@@ -921,7 +1036,9 @@ struct Whole {
                     const double z = ((double)key_f32((uint32_t)(x >> 32)) - (double)largest) / (double)set.t;
                     if (x >= least && x < first && exp(z) >= floor) first = x;
                 });
-                least = block_extreme<false>(first);
+                u64 any = 0;
+                block_extremes(first, any);
+                least = first;
                 total = above(j) + mass_from(least) * sh.unit[j];
             }
         }
@@ -929,23 +1046,23 @@ struct Whole {
             each_listed([&](u64 x) {
                 if (x >= least) atomicAdd(&sh.border[((int)~(uint32_t)x + skip) / kSlice], weight_of(x));
             });
-        if (tid == 0) sh.pick = 0x7fffffff, sh.last = -1;
+        if (tid == 0) sh.last = -1;
         __syncthreads();
-        for (int s = wave; s < slices; s += kSampleWaves) {
-            const SliceHead h = data[s].head;
-            const int below = step_below(h);
-            double m = 0.;
-            for (int j = lane; j < h.used && j + below < edge; j += kWave) m += (double)data[s].whole.mass[j] * sh.unit[j + below];
-            for (int o = 32; o > 0; o >>= 1) m += __shfl_xor(m, o);
-            if (lane == 0) sh.slice[s] = m + (edge < kSteps ? (double)sh.border[s] * sh.unit[edge] : 0.);
-        }
+        double part = 0.;
+        for_slices([&](int s, const SliceHead& h, int below, int j, u64 m, uint32_t) {
+            if (j < h.used && j + below < edge) part += (double)m * sh.unit[j + below];
+        }, [&](int s) {
+            for (int o = 32; o > 0; o >>= 1) part += __shfl_xor(part, o);
+            if (lane == 0) sh.slice[s] = part + (edge < kSteps ? (double)sh.border[s] * sh.unit[edge] : 0.);
+            part = 0.;
+        });
         __syncthreads();
         // every thread finds the slice: the first whose running sum exceeds
         // the target, or by rounding the last that holds anything
         const double target = unit(a.uniform[r]) * total;
         double before = 0.;
         int at = 0;
-        double sum = 0.;
+        sum = 0.;
         for (int s = 0; s < slices; ++s) {
             const double m = sh.slice[s];
             if (m > 0.) {
@@ -957,34 +1074,52 @@ struct Whole {
         }
         constexpr int kEach = kSlice / kSampleThreads;
         const int v0 = at * kSlice + tid * kEach;
-        double w[kEach], mine = 0.;
+        constexpr int kPer = Chunk<T>::kPer;
+        u32x4 raw[kEach / kPer];
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
+        for (int i = 0; i < kEach / kPer; ++i) {
+            raw[i] = u32x4{~0u, ~0u, ~0u, ~0u};
+            if (v0 + i * kPer < a.V + skip) raw[i] = *reinterpret_cast<const u32x4*>(row - skip + v0 + i * kPer);
+        }
+        auto kept_weight = [&](int e) -> double {
             const int v = v0 + e;
-            const uint32_t key = v >= skip && v < a.V + skip ? key_at(row, v - skip) : 0u;
-            const Step st = place(key_f32(max(key, kKeyNone)));   // no token: beyond the steps
-            const bool kept = st.step < kSteps && (st.step < edge || (st.step == edge && ((u64)key << 32 | (uint32_t)~(v - skip)) >= least));
-            w[e] = kept ? (double)weight(st.rest) * sh.unit[min(st.step, kSteps - 1)] : 0.;
-            mine += w[e];
-        }
-        double run = before + block_upto(mine, reinterpret_cast<double*>(tmp)) - mine;
-        int pick = 0x7fffffff, last = -1;
+            const float z = vector_at<T>(raw[e / kPer], e % kPer);
+            const Step st = place(z);   // NaN and -inf: beyond the steps
+            if (v < skip || v >= a.V + skip || st.step >= kSteps || st.step > edge) return 0.;
+            if (st.step == edge && ((u64)logit_key(z) << 32 | (uint32_t)~(v - skip)) < least) return 0.;
+            return (double)weight(st.rest) * sh.unit[st.step];
+        };
+        double mine = 0.;
 #pragma unroll
-        for (int e = kEach - 1; e >= 0; --e)
-            if (w[e] > 0.) last = max(last, v0 + e);
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            run += w[e];
-            if (w[e] > 0. && run > target) pick = min(pick, v0 + e);
-        }
-        if (pick != 0x7fffffff) atomicMin(&sh.pick, pick);
-        if (last >= 0) atomicMax(&sh.last, last);
+        for (int e = 0; e < kEach; ++e) mine += kept_weight(e);
+        const double run = before + block_upto(mine, reinterpret_cast<double*>(tmp));
+        // the first thread whose running sum exceeds the target, or by rounding the last that holds anything
+        const int found = block_min(mine > 0. && run > target ? tid : 0x7fffffff, &sh.cut);
+        if (mine > 0.) atomicMax(&sh.last, tid);
         __syncthreads();
-        if (tid == 0) {
-            const int v = (sh.pick != 0x7fffffff ? sh.pick : sh.last) - skip;
-            a.token[r] = v;
+        const int who = found != 0x7fffffff ? found : sh.last;
+        if (tid == who) tmp[0] = (u64)__double_as_longlong(run - mine);
+        __syncthreads();
+        if (wave != 0) return true;
+        // its logits, one a lane
+        static_assert(kEach <= kWave, "a logit a lane");
+        const int v = at * kSlice + who * kEach + min(lane, kEach - 1);
+        const bool real = lane < kEach && v >= skip && v < a.V + skip;
+        const uint32_t key = real ? key_at(row, v - skip) : 0u;
+        const Step st = place(key_f32(max(key, kKeyNone)));
+        const bool keep = real && st.step < kSteps && (st.step < edge || (st.step == edge && ((u64)key << 32 | (uint32_t)~(v - skip)) >= least));
+        const double w = keep ? (double)weight(st.rest) * sh.unit[min(st.step, kSteps - 1)] : 0.;
+        double upto = w;
+        for (int o = 1; o < kWave; o <<= 1) {
+            const double up = __shfl_up(upto, o);
+            if (lane >= o) upto += up;
+        }
+        upto += __longlong_as_double((long long)tmp[0]);
+        const u64 some = __ballot(w > 0.), over = __ballot(w > 0. && upto > target);
+        if (lane == (over != 0 ? __builtin_ctzll(over) : 63 - __builtin_clzll(some))) {
+            a.token[r] = v - skip;
             if (a.logprob != nullptr)
-                a.logprob[r] = (float)(((double)key_f32(key_at(row, v)) - (double)largest) / (double)set.t - log(total));
+                a.logprob[r] = (float)(((double)key_f32(key) - (double)largest) / (double)set.t - log(total));
         }
         return true;
     }
@@ -1021,7 +1156,7 @@ __global__ __launch_bounds__(kSampleThreads, 4) void pick_kernel(SampleArgs a, i
             }
             return;
         }
-        const double per = 8. / (double)set.t, ytop = (double)largest * per;
+        const double per = kPerUnit / (double)set.t, ytop = (double)largest * per;
         if (fabs(ytop) < kFar) {
             const T* row = static_cast<const T*>(a.logits) + (size_t)r * a.ld;
             const double one = ldexp(1., bits);
