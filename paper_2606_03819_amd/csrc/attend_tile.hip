@@ -55,20 +55,33 @@ __device__ __forceinline__ uint32_t f16_pair(float a, float b) {
 template <int D>
 struct TokenTile {
     u32x4 k[D / 32], v[D / 32];
-    float ks, ev, inv;   // of the lane's half: key scale, value exponent e, 2^-e
-    int left;            // tokens of the lane's half that are real, 16 or less
+    float ks, vs;   // of the lane's half: key scale, value scale
+    int left;       // tokens of the lane's half that are real, 16 or less
+};
+
+// Pages of a wave's next 64 tiles, a tile a lane and each of the tile's halves
+// apart, so that a tile's loads do not wait for its table entry.  A page that
+// is none becomes -1.
+struct TilePages {
+    int id[2];
+    __device__ void load(const AttendArgs& a, const int32_t* table, int t0, int step) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const long long t = (long long)t0 + (long long)lane * step + 16 * h;
+            const int p = table[min((int)(t / a.page), a.max_pages - 1)];
+            id[h] = p >= 0 && p < a.num_pages ? p : -1;
+        }
+    }
 };
 
 template <int D>
-__device__ __forceinline__ void load_tile(TokenTile<D>& t, const AttendArgs& a, const int32_t* table, int hk, int t0,
-                                          int hi, float qscale) {
+__device__ __forceinline__ void load_tile(TokenTile<D>& t, const AttendArgs& a, const TilePages& pages, int nth, int hk,
+                                          int t0, int hi) {
     const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31;
     const int kb = (r >> 2) & 1;
-    int id0 = table[t0 / a.page];
-    int id1 = table[min((t0 + 16) / a.page, a.max_pages - 1)];
-    const bool ok0 = id0 >= 0 && id0 < a.num_pages, ok1 = id1 >= 0 && id1 < a.num_pages;
-    id0 = ok0 ? id0 : 0;   // its tokens count for nothing, and page 0 is there
-    id1 = ok1 ? id1 : 0;
+    const int p0 = __builtin_amdgcn_readlane(pages.id[0], nth), p1 = __builtin_amdgcn_readlane(pages.id[1], nth);
+    const int id0 = max(p0, 0), id1 = max(p1, 0);   // no page: its tokens count for nothing, and page 0 is there
     const int idk = kb ? id1 : id0, idv = half ? id1 : id0;
     const int tk = (t0 + 16 * kb + 4 * (r >> 3) + (r & 3)) & (a.page - 1);
     const int tv = (t0 + 16 * half) & (a.page - 1);
@@ -80,11 +93,9 @@ __device__ __forceinline__ void load_tile(TokenTile<D>& t, const AttendArgs& a, 
         t.k[c] = *reinterpret_cast<const u32x4*>(k + 32 * c);
         t.v[c] = *reinterpret_cast<const u32x4*>(v + (size_t)(32 * c) * a.page);
     }
-    t.ks = a.k_scale[headv] * qscale;
-    const int e = (int)(__float_as_uint(a.v_scale[headv]) >> 23) - 127;
-    t.ev = (float)e;
-    t.inv = __uint_as_float((uint32_t)(127 - e) << 23);
-    t.left = (half ? ok1 : ok0) ? min(max(hi - t0 - 16 * half, 0), 16) : 0;
+    t.ks = a.k_scale[headv];
+    t.vs = a.v_scale[headv];
+    t.left = (half ? p1 : p0) >= 0 ? min(max(hi - t0 - 16 * half, 0), 16) : 0;
 }
 
 // The running softmax of a lane's query row (both halves hold the same m).
@@ -92,12 +103,15 @@ struct Running {
     float m, l;
 };
 
-// u[16] (base 2, -inf: not there) become weights; O^T and l follow a raised m.
+// x[16] become weights 2^(x ks + e - m); O^T and l follow a raised m.  ks is
+// not negative, so the largest x has the largest weight; -inf is not there
+// (ks is 1 then).  `inv`: what the denominator's weights carry, 2^-e.
 template <int D>
-__device__ __forceinline__ void weigh(float (&u)[16], Running& s, f32x16 (&o)[D / 32], float inv) {
-    float top = u[0];
+__device__ __forceinline__ void weigh(float (&x)[16], float ks, float e, float inv, Running& s, f32x16 (&o)[D / 32]) {
+    float top = x[0];
 #pragma unroll
-    for (int j = 1; j < 16; ++j) top = fmaxf(top, u[j]);
+    for (int j = 1; j < 16; ++j) top = fmaxf(top, x[j]);
+    top = fmaf(top, ks, e);
     top = fmaxf(top, lane_xor<32>(top));
     const bool raise = top > s.m + kSlack;   // also from an empty start (-inf)
     if (__any(raise)) {
@@ -109,14 +123,14 @@ __device__ __forceinline__ void weigh(float (&u)[16], Running& s, f32x16 (&o)[D 
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[c][j] *= f;
     }
-    const float m = s.m == neg_inf() ? 0.f : s.m;
+    const float off = s.m == neg_inf() ? 0.f : e - s.m;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-        u[j] = __builtin_amdgcn_exp2f(u[j] - m);
-        sum += u[j];
+        x[j] = __builtin_amdgcn_exp2f(fmaf(x[j], ks, off));
+        sum += x[j];
     }
-    s.l += sum * inv;
+    s.l = fmaf(sum, inv, s.l);
 }
 
 // Workgroup (block of NQ * 32 query rows of a key head, range of the context):
@@ -156,19 +170,31 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
             q[n][c][0] = *reinterpret_cast<const u32x4*>(p + 32 * c);
             q[n][c][1] = *reinterpret_cast<const u32x4*>(p + 32 * c + 8);
             o[n][c] = f32x16{};
+            if (a.scale < 0.f)   // the sign goes to the queries
+#pragma unroll
+                for (int w = 0; w < 4; ++w) q[n][c][0][w] ^= 0x80008000u, q[n][c][1][w] ^= 0x80008000u;
         }
         st[n] = {neg_inf(), 0.f};
     }
-    const float qscale = a.scale * kLog2e;
+    const float qscale = fabsf(a.scale) * kLog2e;
     const int32_t* table = a.block_table + (size_t)s * a.max_pages;
     const int lo = range * sp.chunk, hi = min(ctx, lo + sp.chunk);
     constexpr int kStep = kAttendWaves * 32;
     int t0 = lo + wave * 32;
     TokenTile<D> next;
-    if (t0 < hi) load_tile<D>(next, a, table, hk, t0, hi, qscale);
-    for (; t0 < hi; t0 += kStep) {
+    TilePages pages, later;   // of tiles 64i.. and 64(i+1)..
+    if (t0 < hi) {
+        pages.load(a, table, t0, kStep);
+        later = pages;
+        load_tile<D>(next, a, pages, 0, hk, t0, hi);
+    }
+    for (int nth = 0; t0 < hi; t0 += kStep, ++nth) {
         TokenTile<D> t = next;
-        if (t0 + kStep < hi) load_tile<D>(next, a, table, hk, t0 + kStep, hi, qscale);
+        if (t0 + kStep < hi) {
+            if ((nth & 63) == 0) later.load(a, table, (int)min((long long)t0 + 64 * kStep, (long long)hi - 1), kStep);   // used 63 tiles on
+            if ((nth & 63) == 63) pages = later;
+            load_tile<D>(next, a, pages, (nth + 1) & 63, hk, t0 + kStep, hi);
+        }
         f32x16 acc[NQ];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) acc[n] = f32x16{};
@@ -191,16 +217,22 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
                     t.v[c][w] &= keep == 4 ? ~0u : (1u << (8 * keep)) - 1u;
                 }
         }
+        const int e = (int)(__float_as_uint(t.vs) >> 23) - 127;
+        const float ks = t.ks * qscale, inv = __uint_as_float((uint32_t)(127 - e) << 23);
         u32x4 p[NQ][2];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             float u[16];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) u[j] = acc[n][j] * t.ks + t.ev;
-            if (part)
+            for (int j = 0; j < 16; ++j) u[j] = acc[n][j];
+            float k1 = ks, e1 = (float)e;
+            if (part) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) u[j] = j < t.left ? u[j] : neg_inf();
-            weigh<D>(u, st[n], o[n], t.inv);
+                for (int j = 0; j < 16; ++j) u[j] = j < t.left ? fmaf(u[j], ks, e1) : neg_inf();
+                k1 = 1.f;
+                e1 = 0.f;
+            }
+            weigh<D>(u, k1, e1, inv, st[n], o[n]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) p[n][j >> 2][j & 3] = f16_pair(u[2 * j], u[2 * j + 1]);
         }
@@ -251,7 +283,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
                     sees |= see ? 1u << j : 0u;
                     w[n][j] = see ? acc[n][j] * qscale : neg_inf();
                 }
-                weigh<D>(w[n], st[n], o[n], 1.f);
+                weigh<D>(w[n], 1.f, 0.f, 1.f, st[n], o[n]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const uint32_t h = f32x2_to_bf16x2_bits(w[n][2 * j], w[n][2 * j + 1]);
