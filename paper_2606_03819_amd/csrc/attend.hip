@@ -172,15 +172,33 @@ __global__ __launch_bounds__(kAttendThreads) void merge_kernel(AttendArgs a) {
     const int s = (int)(row / ((size_t)a.n * a.Hq)), i = (int)(row / a.Hq % a.n);
     const int count = split_context(context_of(a, s), a.splits).count;
     if (count == 1 || i >= new_of(a, s)) return;
-    float m = neg_inf(), l = 0.f, o[D / kWave] = {};
-    for (int sp = 0; sp < count; ++sp) {
-        const float* p = part_sums(a, row, sp, D);
-        const float mp = part_stats(a, row, sp, D)[0], lp = part_stats(a, row, sp, D)[1];
-        if (lp == 0.f) continue;
-        const float mn = fmaxf(m, mp), fa = exp2f(m - mn), fb = exp2f(mp - mn);
-        m = mn;
-        l = l * fa + lp * fb;
-        for (int c = 0; c < D / kWave; ++c) o[c] = o[c] * fa + p[c * kWave + lane] * fb;
+    // every range's factor first, a range a lane
+    static_assert(kMostSplits <= kWave, "a range a lane");
+    float mp = neg_inf(), lp = 0.f;
+    if (lane < count) {
+        const float* ml = part_stats(a, row, lane, D);
+        mp = ml[0];
+        lp = ml[1];
+    }
+    const float m = wave_max(mp);
+    const float f = mp == neg_inf() ? (lp == 0.f ? 0.f : lp) : exp2f(mp - m);   // a sum that is no number stays one
+    const float l = wave_sum(lp * f);
+    float o[D / kWave] = {};
+    constexpr int kDeep = 8;
+    for (int s0 = 0; s0 < count; s0 += kDeep) {
+        float x[kDeep][D / kWave];
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i)
+#pragma unroll
+            for (int c = 0; c < D / kWave; ++c)
+                x[i][c] = s0 + i < count ? part_sums(a, row, s0 + i, D)[c * kWave + lane] : 0.f;
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) {
+            const float g = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), s0 + i));
+#pragma unroll
+            for (int c = 0; c < D / kWave; ++c)
+                if (s0 + i < count && g != 0.f) o[c] += x[i][c] * g;
+        }
     }
     for (int c = 0; c < D / kWave; ++c) store_out(a.out, row * D + c * kWave + lane, l == 0.f ? 0.f : o[c] / l, sizeof(T) == 2);
     if (lane == 0 && a.lse != nullptr) a.lse[row] = lse_of(m, l);
@@ -188,19 +206,26 @@ __global__ __launch_bounds__(kAttendThreads) void merge_kernel(AttendArgs a) {
 
 namespace {
 
-// Ranges a context is split into at most: enough for about 1024 workgroups.
-int most_splits(long long groups, int max_pages, int page) {
+// Ranges a context is split into at most.  `groups` workgroups serve one range
+// and `slots` of them run at once.  Few groups are split to fill the slots
+// once (a second round of mostly idle units costs what the first does: 24
+// groups over 8192 tokens 32 us against 37); many are split so that uneven
+// contexts spread over two rounds or more (384 groups over up to 16384 tokens:
+// 239 us in two ranges, 218 in three, 227 in four, and the partial sums grow).
+int most_splits(long long groups, int slots, int max_pages, int page) {
     const long long longest = ((long long)max_pages * page + kSplitLeast - 1) / kSplitLeast;
-    long long want = (1024 + groups - 1) / groups;
+    long long want = groups * 2 <= slots ? slots / groups : (2 * slots + groups - 1) / groups;
     want = want < longest ? want : longest;
-    return (int)(want < 1 ? 1 : want > 64 ? 64 : want);
+    return (int)(want < 1 ? 1 : want > kMostSplits ? kMostSplits : want);
 }
 
 int row_blocks(int Hq, int Hkv) { return (Hq / Hkv + kGroupRows - 1) / kGroupRows; }
 
 int splits_of(int b, int n, int Hq, int Hkv, int page, int max_pages, bool bf16) {
-    const long long groups = bf16 ? (long long)b * Hkv * tile_blocks(n, Hq, Hkv) : (long long)b * n * Hkv * row_blocks(Hq, Hkv);
-    return most_splits(groups, max_pages, page);
+    // workgroups on 256 CUs: four where a wave keeps one row tile or fp32 sums, two where it keeps more
+    if (!bf16) return most_splits((long long)b * n * Hkv * row_blocks(Hq, Hkv), 1024, max_pages, page);
+    const TileBlocks tb = tile_blocks(n, Hq, Hkv);
+    return most_splits((long long)b * Hkv * tb.blocks, tb.tiles == 1 ? 1024 : 512, max_pages, page);
 }
 
 template <class T>

@@ -13,7 +13,7 @@ constexpr int kGroupRows = 4;   // query heads of one position that a workgroup 
 
 // The ranges that a context of `ctx` tokens is split into: at most `most`, of
 // kSplitLeast tokens at least, each a multiple of 64 but the last.
-constexpr int kSplitLeast = 256;
+constexpr int kSplitLeast = 256, kMostSplits = 64;
 struct Split {
     int chunk, count;
 };
@@ -53,8 +53,11 @@ __device__ __forceinline__ void store_out(void* out, size_t at, float v, bool bf
 // A finished row: sums over weights (none: zeros and -inf).
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? neg_inf() : (m + __log2f(l)) * kLn2; }
 
-// Blocks of 32 query rows that a key head's positions make.
-int tile_blocks(int n, int Hq, int Hkv);
+// Blocks of query rows that a key head's positions make, and row tiles a block.
+struct TileBlocks {
+    int blocks, tiles;
+};
+TileBlocks tile_blocks(int n, int Hq, int Hkv);
 hipError_t launch_attend_tile(const AttendArgs& a, int D, hipStream_t stream);
 
 }  // namespace tf
