@@ -439,14 +439,37 @@ def treeflash_accept(tree: Dict[str, torch.Tensor], target: torch.Tensor, gamma:
 E4M3 = torch.float8_e4m3fn
 
 
+# as with the stream: torch keeps the cheap form of torch.cuda.current_device() private
+_device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _launch(func: str, dev, *args):
     """Calls the library with `dev` the current device (its streams belong to it) and `dev`'s current stream."""
     f = getattr(lib(), func)
-    if dev.index is None or torch.cuda.current_device() == dev.index:
+    if dev.index is None or _device_now() == dev.index:
         _check(func, f(*args, _stream(dev)))
     else:
         with torch.cuda.device(dev):
             _check(func, f(*args, _stream(dev)))
+
+
+def _arg(func: str, name: str, t: Optional[torch.Tensor], dtype, shape: tuple, dev) -> Optional[int]:
+    """Pointer of a dense tensor of this type, shape and device; the errors of _ptr and _shapes otherwise."""
+    if t is None:
+        return None
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous():
+        return t.data_ptr()
+    ptr = _ptr(t, name, dtype, dev)
+    _shapes(func, **{name: (t, shape)})
+    return ptr
+
+
+def _gpu(name: str, t) -> torch.device:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    return t.device
 
 
 def _rows_ptr(t: torch.Tensor, name: str, inner: int, dtype, device) -> tuple:
@@ -484,25 +507,27 @@ def treeflash_sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: O
     """A token for every position from logits [b, n, V] (rows may be padded) and random numbers uniform [b, n]
     in [0, 1); temperature, top_k, top_p and min_p are [b] or None (off).  Returns token [b, n] int32, which is
     treeflash_accept's target, and its log-probability among the kept tokens [b, n]."""
+    func = "treeflash_sample"
+    dev = _gpu("logits", logits)
     b, n, V = logits.shape
-    dev = logits.device
-    _shapes("treeflash_sample", uniform=(uniform, (b, n)), temperature=(temperature, (b,)), top_k=(top_k, (b,)),
-            top_p=(top_p, (b,)), min_p=(min_p, (b,)), token=(token, (b, n)), logprob=(logprob, (b, n)))
     dt = _dtype_code(logits)
+    i32, f32, rows = torch.int32, torch.float32, (b, n)
     ptr, ld = _rows_ptr(logits, "logits", 1, logits.dtype, dev)
+    args = (_arg(func, "temperature", temperature, f32, (b,), dev), _arg(func, "top_k", top_k, i32, (b,), dev),
+            _arg(func, "top_p", top_p, f32, (b,), dev), _arg(func, "min_p", min_p, f32, (b,), dev),
+            _arg(func, "uniform", uniform, f32, rows, dev))
     if token is None:
-        token = torch.empty((b, n), dtype=torch.int32, device=dev)
+        token = torch.empty(rows, dtype=i32, device=dev)
     if logprob is None:
-        logprob = torch.empty((b, n), dtype=torch.float32, device=dev)
+        logprob = torch.empty(rows, dtype=f32, device=dev)
     if workspace is None:
         workspace = alloc_workspace(treeflash_sample_workspace_bytes(b, n, V), dev)
-    f32 = torch.float32
-    _launch("treeflash_sample", dev, ptr, ld, b, n, V, dt, _ptr(temperature, "temperature", f32, dev),
-            _ptr(top_k, "top_k", torch.int32, dev), _ptr(top_p, "top_p", f32, dev), _ptr(min_p, "min_p", f32, dev),
-            _ptr(uniform, "uniform", f32, dev), _ptr(token, "token", torch.int32, dev),
-            _ptr(logprob, "logprob", f32, dev), _ptr(workspace, "workspace", device=dev),
-            workspace.numel() * workspace.element_size())
+    _launch(func, dev, ptr, ld, b, n, V, dt, *args, _arg(func, "token", token, i32, rows, dev),
+            _arg(func, "logprob", logprob, f32, rows, dev), _ptr(workspace, "workspace", device=dev), workspace.nbytes)
     return token, logprob
+
+
+_SLOTS_OUT = ("context_len", "free_count", "start", "page_start", "slot", "position", "source", "status")
 
 
 def treeflash_cache_slots(context_len: torch.Tensor, add_len: torch.Tensor, free_pages: torch.Tensor,
@@ -512,51 +537,54 @@ def treeflash_cache_slots(context_len: torch.Tensor, add_len: torch.Tensor, free
     tokens, or with `accepted` [b, gamma] (treeflash_accept's, add_len its accept_len) the root and the accepted
     nodes of a tree input of n positions.  block_table is updated in place.  `out` may hold context_len and
     free_count themselves to update them in place; status 0 says that the pages sufficed."""
+    func = "treeflash_cache_slots"
+    dev = _gpu("block_table", block_table)
     b, max_pages = block_table.shape
-    dev = block_table.device
     i32 = torch.int32
     gamma = accepted.shape[1] if accepted is not None else 0
-    if out is None:
-        e = dict(dtype=i32, device=dev)
-        out = {"context_len": torch.empty((b,), **e), "free_count": torch.empty((1,), **e),
-               "start": torch.empty((b + 1,), **e), "page_start": torch.empty((b + 1,), **e),
-               "slot": torch.empty((max_tokens,), **e), "position": torch.empty((max_tokens,), **e),
-               "source": torch.empty((max_tokens,), **e), "status": torch.empty((1,), **e)}
+    max_free = free_pages.numel()
+    args = (_arg(func, "context_len", context_len, i32, (b,), dev), _arg(func, "add_len", add_len, i32, (b,), dev),
+            _arg(func, "accepted", accepted, i32, (b, gamma), dev),
+            _arg(func, "free_pages", free_pages, i32, (max_free,), dev),
+            _arg(func, "free_count", free_count, i32, (1,), dev), b, gamma, n, page_size, max_pages, max_free, max_tokens,
+            _arg(func, "block_table", block_table, i32, (b, max_pages), dev))
+    sizes = (b, 1, b + 1, b + 1, max_tokens, max_tokens, max_tokens, 1)
+    if out is None:   # one allocation for all of them
+        if max_tokens < 1:
+            raise ValueError(f"{func}: max_tokens must be positive")
+        parts = torch.empty((sum(sizes),), dtype=i32, device=dev).split(sizes)
+        out = dict(zip(_SLOTS_OUT, parts))
+        outs = [p.data_ptr() for p in parts]
+    else:
+        outs = [_arg(func, f, out.get(f), i32, (size,), dev) for f, size in zip(_SLOTS_OUT, sizes)]
     out["block_table"] = block_table
-    _shapes("treeflash_cache_slots", context_len=(context_len, (b,)), add_len=(add_len, (b,)),
-            accepted=(accepted, (b, gamma)), free_pages=(free_pages, (free_pages.numel(),)),
-            free_count=(free_count, (1,)), new_len=(out["context_len"], (b,)), new_count=(out["free_count"], (1,)),
-            start=(out["start"], (b + 1,)), page_start=(out["page_start"], (b + 1,)),
-            slot=(out["slot"], (max_tokens,)), position=(out.get("position"), (max_tokens,)),
-            source=(out.get("source"), (max_tokens,)), status=(out["status"], (1,)))
-    _launch("treeflash_cache_slots", dev, _ptr(context_len, "context_len", i32, dev), _ptr(add_len, "add_len", i32, dev),
-            _ptr(accepted, "accepted", i32, dev), _ptr(free_pages, "free_pages", i32, dev),
-            _ptr(free_count, "free_count", i32, dev), b, gamma, n, page_size, max_pages, free_pages.numel(), max_tokens,
-            _ptr(block_table, "block_table", i32, dev),
-            *[_ptr(out.get(f), f, i32, dev) for f in ("context_len", "free_count", "start", "page_start", "slot",
-                                                      "position", "source", "status")])
+    _launch(func, dev, *args, *outs)
     return out
 
 
 def treeflash_cache_release(done: torch.Tensor, context_len: torch.Tensor, block_table: torch.Tensor,
                             free_pages: torch.Tensor, free_count: torch.Tensor, page_size: int):
     """Gives the pages of the sequences with done [b] (uint8) back; lengths, stack and count change in place."""
+    func = "treeflash_cache_release"
+    dev = _gpu("block_table", block_table)
     b, max_pages = block_table.shape
-    dev = block_table.device
-    i32 = torch.int32
-    _shapes("treeflash_cache_release", done=(done, (b,)), context_len=(context_len, (b,)),
-            free_pages=(free_pages, (free_pages.numel(),)), free_count=(free_count, (1,)))
-    ln, fc = _ptr(context_len, "context_len", i32, dev), _ptr(free_count, "free_count", i32, dev)
-    _launch("treeflash_cache_release", dev, _ptr(done, "done", torch.uint8, dev), ln,
-            _ptr(block_table, "block_table", i32, dev), fc, b, page_size, max_pages, free_pages.numel(),
-            _ptr(free_pages, "free_pages", i32, dev), ln, fc)
+    i32, max_free = torch.int32, free_pages.numel()
+    ln = _arg(func, "context_len", context_len, i32, (b,), dev)
+    fc = _arg(func, "free_count", free_count, i32, (1,), dev)
+    _launch(func, dev, _arg(func, "done", done, torch.uint8, (b,), dev), ln,
+            _arg(func, "block_table", block_table, i32, (b, max_pages), dev), fc, b, page_size, max_pages, max_free,
+            _arg(func, "free_pages", free_pages, i32, (max_free,), dev), ln, fc)
 
 
-def _cache_shapes(func: str, k_cache, v_cache, k_scale, v_scale, Hkv: int, D: int):
-    num_pages, _, page_size, _ = k_cache.shape
-    _shapes(func, k_cache=(k_cache, (num_pages, Hkv, page_size, D)), v_cache=(v_cache, (num_pages, Hkv, D, page_size)),
-            k_scale=(k_scale, (num_pages, Hkv)), v_scale=(v_scale, (num_pages, Hkv)))
-    return num_pages, page_size
+def _cache_args(func: str, k_cache, v_cache, k_scale, v_scale, Hkv: int, D: int, dev):
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError(f"{func}: k_cache must be [pages, heads, page_size, head size]")
+    pages, _, page, _ = k_cache.shape
+    f32 = torch.float32
+    return pages, page, (_arg(func, "k_cache", k_cache, E4M3, (pages, Hkv, page, D), dev),
+                         _arg(func, "v_cache", v_cache, E4M3, (pages, Hkv, D, page), dev),
+                         _arg(func, "k_scale", k_scale, f32, (pages, Hkv), dev),
+                         _arg(func, "v_scale", v_scale, f32, (pages, Hkv), dev))
 
 
 def treeflash_cache_append(k_new: torch.Tensor, v_new: torch.Tensor, slot: torch.Tensor, k_cache: torch.Tensor,
@@ -565,22 +593,22 @@ def treeflash_cache_append(k_new: torch.Tensor, v_new: torch.Tensor, slot: torch
     """Writes keys and values [..., Hkv, D] into the cache: row source[i] (None: i) to slot[i], -1 none.  The
     rows may be views of a wider projection.  Caches are float8_e4m3fn, k [pages, Hkv, page_size, D], v
     [pages, Hkv, D, page_size], scales [pages, Hkv] fp32; all four change in place."""
+    func = "treeflash_cache_append"
+    dev = _gpu("k_cache", k_cache)
     Hkv, D = k_new.shape[-2:]
-    dev = k_cache.device
-    num_pages, page_size = _cache_shapes("treeflash_cache_append", k_cache, v_cache, k_scale, v_scale, Hkv, D)
-    N = slot.numel()
-    _shapes("treeflash_cache_append", v_new=(v_new, k_new.shape), slot=(slot, (N,)), source=(source, (N,)))
+    pages, page, cache = _cache_args(func, k_cache, v_cache, k_scale, v_scale, Hkv, D, dev)
+    N, i32 = slot.numel(), torch.int32
+    if v_new.shape != k_new.shape:
+        raise ValueError(f"{func}: v_new has shape {tuple(v_new.shape)}, expected {tuple(k_new.shape)}")
     dt = _dtype_code(k_new)
     kp, ld = _rows_ptr(k_new, "k_new", 2, k_new.dtype, dev)
     vp, ldv = _rows_ptr(v_new, "v_new", 2, k_new.dtype, dev)
     if ld != ldv:
-        raise ValueError("treeflash_cache_append: k_new and v_new must have the same strides")
+        raise ValueError(f"{func}: k_new and v_new must have the same strides")
+    slots, sources = _arg(func, "slot", slot, i32, (N,), dev), _arg(func, "source", source, i32, (N,), dev)
     if N == 0 or k_new.numel() == 0:
         return
-    _launch("treeflash_cache_append", dev, kp, vp, ld, k_new.numel() // (Hkv * D), _ptr(slot, "slot", torch.int32, dev),
-            _ptr(source, "source", torch.int32, dev), N, Hkv, D, page_size, num_pages, dt,
-            _ptr(k_cache, "k_cache", E4M3, dev), _ptr(v_cache, "v_cache", E4M3, dev),
-            _ptr(k_scale, "k_scale", torch.float32, dev), _ptr(v_scale, "v_scale", torch.float32, dev))
+    _launch(func, dev, kp, vp, ld, k_new.numel() // (Hkv * D), slots, sources, N, Hkv, D, page, pages, dt, *cache)
 
 
 def treeflash_tree_attention_workspace_bytes(b, n, Hq, Hkv, D, page_size, max_pages, dtype) -> int:
@@ -597,35 +625,34 @@ def treeflash_tree_attention(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.
     k_new and v_new [b, n, Hkv, D], as mask [b, n, n] (uint8, treeflash_tree_attention_inputs) admits them
     (None: positions up to their own).  q, k_new and v_new may be views of one projection's rows.  Returns
     out [b, n, Hq, D] and lse [b, n, Hq]; positions from new_len[s] on stay as they were."""
-    b, n, Hq, D = q.shape
-    Hkv = k_new.shape[2]
-    dev = q.device
-    max_pages = block_table.shape[1]
     func = "treeflash_tree_attention"
-    num_pages, page_size = _cache_shapes(func, k_cache, v_cache, k_scale, v_scale, Hkv, D)
-    _shapes(func, k_new=(k_new, (b, n, Hkv, D)), v_new=(v_new, (b, n, Hkv, D)), mask=(mask, (b, n, n)),
-            context_len=(context_len, (b,)), block_table=(block_table, (b, max_pages)), new_len=(new_len, (b,)),
-            out=(out, (b, n, Hq, D)), lse=(lse, (b, n, Hq)))
+    dev = _gpu("q", q)
+    b, n, Hq, D = q.shape
+    Hkv, max_pages, dtype = k_new.shape[2], block_table.shape[1], q.dtype
+    pages, page, cache = _cache_args(func, k_cache, v_cache, k_scale, v_scale, Hkv, D, dev)
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        if t.shape != (b, n, Hkv, D):
+            raise ValueError(f"{func}: {name} has shape {tuple(t.shape)}, expected {(b, n, Hkv, D)}")
     dt = _dtype_code(q)
-    qp, ldq = _rows_ptr(q, "q", 2, q.dtype, dev)
-    kp, ld = _rows_ptr(k_new, "k_new", 2, q.dtype, dev)
-    vp, ldv = _rows_ptr(v_new, "v_new", 2, q.dtype, dev)
+    qp, ldq = _rows_ptr(q, "q", 2, dtype, dev)
+    kp, ld = _rows_ptr(k_new, "k_new", 2, dtype, dev)
+    vp, ldv = _rows_ptr(v_new, "v_new", 2, dtype, dev)
     if ld != ldv:
         raise ValueError(f"{func}: k_new and v_new must have the same strides")
+    i32, f32 = torch.int32, torch.float32
+    args = (_arg(func, "mask", mask, torch.uint8, (b, n, n), dev), _arg(func, "new_len", new_len, i32, (b,), dev),
+            _arg(func, "context_len", context_len, i32, (b,), dev),
+            _arg(func, "block_table", block_table, i32, (b, max_pages), dev), *cache)
     if out is None:
-        out = torch.empty((b, n, Hq, D), dtype=q.dtype, device=dev)
+        out = torch.empty((b, n, Hq, D), dtype=dtype, device=dev)
     if lse is None:
-        lse = torch.empty((b, n, Hq), dtype=torch.float32, device=dev)
+        lse = torch.empty((b, n, Hq), dtype=f32, device=dev)
     if workspace is None:
         workspace = alloc_workspace(
-            treeflash_tree_attention_workspace_bytes(b, n, Hq, Hkv, D, page_size, max_pages, dt), dev)
-    i32, f32 = torch.int32, torch.float32
-    _launch(func, dev, qp, ldq, kp, vp, ld, _ptr(mask, "mask", torch.uint8, dev), _ptr(new_len, "new_len", i32, dev),
-            _ptr(context_len, "context_len", i32, dev), _ptr(block_table, "block_table", i32, dev),
-            _ptr(k_cache, "k_cache", E4M3, dev), _ptr(v_cache, "v_cache", E4M3, dev), _ptr(k_scale, "k_scale", f32, dev),
-            _ptr(v_scale, "v_scale", f32, dev), b, n, Hq, Hkv, D, page_size, max_pages, num_pages, float(scale), dt,
-            _ptr(out, "out", q.dtype, dev), _ptr(lse, "lse", f32, dev), _ptr(workspace, "workspace", device=dev),
-            workspace.numel() * workspace.element_size())
+            treeflash_tree_attention_workspace_bytes(b, n, Hq, Hkv, D, page, max_pages, dt), dev)
+    _launch(func, dev, qp, ldq, kp, vp, ld, *args, b, n, Hq, Hkv, D, page, max_pages, pages, float(scale), dt,
+            _arg(func, "out", out, dtype, (b, n, Hq, D), dev), _arg(func, "lse", lse, f32, (b, n, Hq), dev),
+            _ptr(workspace, "workspace", device=dev), workspace.nbytes)
     return out, lse
 
 

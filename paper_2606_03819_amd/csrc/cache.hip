@@ -35,20 +35,21 @@ __device__ __forceinline__ long long block_scan(long long v, long long* tmp) {
 // Places tokens [i0, i1) of the lists.  `start` and `page_start` are whole
 // and new_len, new_free_count written: the old length of a sequence is its
 // new one less its tokens, and its pages sit below the old top of the stack.
-__device__ void fill_slots(const SlotsArgs& a, int i0, int i1, int step) {
-    const int total = a.start[a.b];
-    const int top = a.new_free_count[0] + a.page_start[a.b];   // pages on the stack before the call
+__device__ __forceinline__ void fill_slots(const SlotsArgs& a, const int32_t* start, const int32_t* page_start, int i0,
+                                           int i1, int step) {
+    const int total = start[a.b];
+    const int top = a.new_free_count[0] + page_start[a.b];   // pages on the stack before the call
     for (int i = i0; i < i1; i += step) {
         int sl = -1, ps = -1, src = -1;
         if (i < total) {
             int lo = 0, hi = a.b;   // start[lo] <= i < start[hi]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (a.start[mid] <= i) lo = mid;
+                if (start[mid] <= i) lo = mid;
                 else hi = mid;
             }
-            const int s = lo, j = i - a.start[s];
-            const int ctx = a.new_len[s] - (a.start[s + 1] - a.start[s]);
+            const int s = lo, j = i - start[s];
+            const int ctx = a.new_len[s] - (start[s + 1] - start[s]);
             ps = ctx + j;
             const int col = ps / a.page, off = ps - col * a.page;
             const int had = pages_of(ctx, a.page);
@@ -57,7 +58,7 @@ __device__ void fill_slots(const SlotsArgs& a, int i0, int i1, int step) {
             if (col < had) {
                 id = a.block_table[at];
             } else {
-                id = a.free_pages[top - 1 - (a.page_start[s] + col - had)];
+                id = a.free_pages[top - 1 - (page_start[s] + col - had)];
                 if (off == 0) a.block_table[at] = id;   // a new page's first token is a new token
             }
             const long long slot = (long long)id * a.page + off;
@@ -75,81 +76,97 @@ __device__ void fill_slots(const SlotsArgs& a, int i0, int i1, int step) {
 
 // One workgroup: sums of tokens and pages over the sequences, whether all of
 // them fit, then lengths and list offsets; `alone`: the lists as well.  What
-// bounds it is the chain of loads and two scans, about a launch.  All reads of
-// lengths and count end before the first write (new_len and new_free_count
-// may be the same arrays).
+// bounds it is a chain of loads and scans, so a batch of up to kPlanThreads
+// sequences is read and scanned once and its offsets are kept in LDS for the
+// lists.  All reads of lengths and count end before the first write (new_len
+// and new_free_count may be the same arrays).
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(SlotsArgs a, int alone) {
     __shared__ long long tmp[kPlanThreads / 64];
     __shared__ long long carry_tok, carry_page;
     __shared__ int bad;
+    __shared__ int32_t s_start[kPlanThreads + 1], s_page[kPlanThreads + 1];
     const int tid = threadIdx.x;
     const int extra = a.accepted != nullptr ? 1 : 0;
-    if (tid == 0) bad = 0, carry_tok = 0, carry_page = 0;
-    __syncthreads();
+    const bool once = a.b <= kPlanThreads;
+    if (tid == 0) bad = 0;
     const int left = a.free_count[0];
     long long tok = 0, pg = 0;
     int wrong = left < 0 || left > a.max_free ? 1 : 0, wide = 0;
+    int ctx = 0, add = 0, need = 0;
     for (int s = tid; s < a.b; s += kPlanThreads) {
-        const int ctx = a.context_len[s], add = a.add_len[s];
+        ctx = a.context_len[s];
+        add = a.add_len[s];
+        need = 0;
         if (ctx < 0 || add < 0 || (extra && add > a.gamma) || (a.n > 0 && (long long)add + extra > a.n)) {
             wrong = 1;
             continue;
         }
-        const long long after = (long long)ctx + add + extra;
-        tok += add + extra;
+        add += extra;   // below 2^31: a.gamma bounds it where extra is 1
+        const long long after = (long long)ctx + add;
+        tok += add;
         if (after > (long long)a.max_pages * a.page) {
             wide = 1;
             continue;
         }
-        pg += pages_of((int)after, a.page) - pages_of(ctx, a.page);
+        need = pages_of((int)after, a.page) - pages_of(ctx, a.page);
+        pg += need;
     }
+    __syncthreads();
     if (wrong) atomicOr(&bad, 1);
     if (wide) atomicOr(&bad, 2);
-    tok = block_scan(tok, tmp);
-    pg = block_scan(pg, tmp);
-    if (tid == kPlanThreads - 1) carry_tok = tok, carry_page = pg;
+    const long long upto_tok = block_scan(tok, tmp), upto_page = block_scan(pg, tmp);
+    if (tid == kPlanThreads - 1) carry_tok = upto_tok, carry_page = upto_page;
     __syncthreads();
     const long long all_tok = carry_tok, all_page = carry_page;
     const int status = (bad & 1) ? 1 : all_tok > a.max_tokens ? 2 : (bad & 2) ? 3 : all_page > left ? 4 : 0;
-    __syncthreads();
     if (tid == 0) {
-        carry_tok = carry_page = 0;
         a.status[0] = status;
-        a.start[0] = 0;
-        a.page_start[0] = 0;
+        a.start[0] = s_start[0] = 0;
+        a.page_start[0] = s_page[0] = 0;
         a.new_free_count[0] = status == 0 ? left - (int)all_page : left;
     }
-    for (int s0 = 0; s0 < a.b; s0 += kPlanThreads) {
-        const int s = s0 + tid;
-        int ctx = 0, add = 0, need = 0;
-        if (s < a.b) {
-            ctx = a.context_len[s];
-            if (status == 0) {
-                add = a.add_len[s] + extra;
-                need = pages_of(ctx + add, a.page) - pages_of(ctx, a.page);
+    if (once) {
+        if (tid < a.b) {
+            a.start[tid + 1] = s_start[tid + 1] = status == 0 ? (int)upto_tok : 0;
+            a.page_start[tid + 1] = s_page[tid + 1] = status == 0 ? (int)upto_page : 0;
+            a.new_len[tid] = status == 0 ? ctx + add : ctx;
+        }
+    } else {
+        __syncthreads();
+        if (tid == 0) carry_tok = carry_page = 0;
+        for (int s0 = 0; s0 < a.b; s0 += kPlanThreads) {
+            const int s = s0 + tid;
+            ctx = add = need = 0;
+            if (s < a.b) {
+                ctx = a.context_len[s];
+                if (status == 0) {
+                    add = a.add_len[s] + extra;
+                    need = pages_of(ctx + add, a.page) - pages_of(ctx, a.page);
+                }
             }
+            const long long t = block_scan(add, tmp), p = block_scan(need, tmp);
+            const long long bt = carry_tok, bp = carry_page;   // written before the scans' barriers
+            if (s < a.b) {
+                a.start[s + 1] = (int)(bt + t);
+                a.page_start[s + 1] = (int)(bp + p);
+                a.new_len[s] = ctx + add;
+            }
+            __syncthreads();
+            if (tid == kPlanThreads - 1) carry_tok = bt + t, carry_page = bp + p;
+            __syncthreads();
         }
-        const long long t = block_scan(add, tmp), p = block_scan(need, tmp);
-        const long long bt = carry_tok, bp = carry_page;   // written before the scans' barriers
-        if (s < a.b) {
-            a.start[s + 1] = (int)(bt + t);
-            a.page_start[s + 1] = (int)(bp + p);
-            a.new_len[s] = ctx + add;
-        }
-        __syncthreads();
-        if (tid == kPlanThreads - 1) carry_tok = bt + t, carry_page = bp + p;
-        __syncthreads();
     }
     if (alone) {
         __threadfence_block();
         __syncthreads();
-        fill_slots(a, tid, a.max_tokens, kPlanThreads);
+        if (once) fill_slots(a, s_start, s_page, tid, a.max_tokens, kPlanThreads);
+        else fill_slots(a, a.start, a.page_start, tid, a.max_tokens, kPlanThreads);
     }
 }
 
 __global__ __launch_bounds__(kFillThreads) void cache_fill_kernel(SlotsArgs a) {
     const int i0 = blockIdx.x * (kFillThreads * kFillPer);
-    fill_slots(a, i0 + threadIdx.x, min(i0 + kFillThreads * kFillPer, a.max_tokens), kFillThreads);
+    fill_slots(a, a.start, a.page_start, i0 + threadIdx.x, min(i0 + kFillThreads * kFillPer, a.max_tokens), kFillThreads);
 }
 
 // One workgroup: the finished sequences' pages go onto the stack in order.
@@ -185,66 +202,96 @@ __global__ __launch_bounds__(kPlanThreads) void cache_release_kernel(ReleaseArgs
 
 constexpr int kAppendThreads = 256;
 
-template <class T>
-__device__ __forceinline__ void load8(const T* p, float* x);
-template <>
-__device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float* x) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = bf16_bits_to_f32(w[i] & 0xffffu);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* x) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-}
-
 __device__ __forceinline__ float finite_abs(float x) {
     const float a = fabsf(x);
     return a < __builtin_inff() ? a : 0.f;   // neither infinities nor NaN enter the scale
 }
 
+// Four tokens' eight dimensions that a thread turns into codes.
+template <class T>
+struct TokenQuad {
+    static constexpr int kWords = sizeof(T) * 8 / 16;
+    u32x4 raw[4][kWords];
+    __device__ void load(const T* rows, long long ld, const int (&row)[4]) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+                raw[t][w] = u32x4{};
+                if (row[t] >= 0) raw[t][w] = reinterpret_cast<const u32x4*>(rows + (size_t)row[t] * ld)[w];
+            }
+    }
+    __device__ float at(int t, int e) const {
+        if (sizeof(T) == 4) return __uint_as_float(raw[t][(e >> 2) & (kWords - 1)][e & 3]);
+        const uint32_t w = raw[t][0][e >> 1];
+        return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+    }
+    __device__ float largest() const {
+        float m = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_abs(at(t, e)));
+        return m;
+    }
+};
+
 // Workgroup (`per` tokens of the list, head): for each run that begins among
 // its tokens, the run's largest values, the scale, what the page held rounded
 // again where the scale rose, the new codes.  The page's first token of the
 // list leads its run, so every page and head has one writer and no atomics.
-// The rows are read twice, the second time from the cache.  Values are turned
-// in LDS, so that the [D, page] side stores dwords of four tokens.
+// A thread takes four tokens' eight dimensions (tokens 4q..4q+3 of the page),
+// all loads in flight at once: four conversions then give a dword along the
+// dimensions for the keys, and one along the tokens for the values' [D, page]
+// side, without a turn through LDS.  Bound by memory latency up to a few
+// pages a CU, by the reads and writes beyond.
 template <class T, int D>
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs a, int per) {
-    constexpr int kChunks = D / 8;                          // threads across a row
-    constexpr int kRowsPass = kAppendThreads / kChunks;
-    constexpr int kPitch = 128 + 4;                         // tokens of a page and a dword, against bank conflicts
-    __shared__ __align__(16) uint8_t turned[D * kPitch];
+    constexpr int kChunks = D / 8;                        // threads across a row
+    constexpr int kQuads = kAppendThreads / kChunks;      // quads of tokens a pass
     __shared__ float s_max[2][kAppendThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int h = blockIdx.y;
     const int end = (int)min((long long)a.N, (long long)(blockIdx.x + 1) * per);
     const long long limit = (long long)a.num_pages * a.page;
-    const int c8 = (tid % kChunks) * 8, r0 = tid / kChunks;
+    const int c8 = (tid % kChunks) * 8;
     const T* kn = static_cast<const T*>(a.k_new) + (size_t)h * D + c8;
     const T* vn = static_cast<const T*>(a.v_new) + (size_t)h * D + c8;
-    for (int i = (int)blockIdx.x * per; i < end; ++i) {     // uniform over the workgroup
+    // the tokens that lead a run, all looked at at once (per <= 64)
+    const int mine = (int)blockIdx.x * per + lane;
+    bool leads = false;
+    if (lane < per && mine < end) {
+        const int sl = a.slot[mine], before = mine > 0 ? a.slot[mine - 1] : -1;
+        leads = sl >= 0 && sl < limit && ((sl & (a.page - 1)) == 0 || before != sl - 1);
+    }
+    for (unsigned long long todo = __ballot(leads); todo != 0; todo &= todo - 1) {   // uniform over the workgroup
+        const int i = (int)blockIdx.x * per + __builtin_ctzll(todo);
         const int sl = a.slot[i];
-        if (sl < 0 || sl >= limit) continue;
         const int off = sl & (a.page - 1), id = sl / a.page;
-        if (off != 0 && i > 0 && a.slot[i - 1] == sl - 1) continue;
         const int most = min(a.page - off, a.N - i);
         const unsigned long long b0 = __ballot(lane < most && a.slot[i + min(lane, most - 1)] == sl + lane);
         const unsigned long long b1 = __ballot(lane + 64 < most && a.slot[i + min(lane + 64, most - 1)] == sl + lane + 64);
         const int run = ~b0 != 0 ? __builtin_ctzll(~b0) : (~b1 != 0 ? 64 + __builtin_ctzll(~b1) : 128);
 
+        const int q0 = off / 4, passes = ((off + run + 3) / 4 - q0 + kQuads - 1) / kQuads;
+        TokenQuad<T> x, y;
+        auto load = [&](int pass) {
+            const int o = 4 * (q0 + pass * kQuads + tid / kChunks) - off;   // the quad's first token, in the run
+            int row[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                row[t] = -1;
+                if (o + t >= 0 && o + t < run) row[t] = a.source != nullptr ? a.source[i + o + t] : i + o + t;
+                if (row[t] >= a.rows) row[t] = -1;
+            }
+            x.load(kn, a.ld_new, row);
+            y.load(vn, a.ld_new, row);
+        };
         float mk = 0.f, mv = 0.f;
-        for (int j = r0; j < run; j += kRowsPass) {
-            const int row = a.source != nullptr ? a.source[i + j] : i + j;
-            if (row < 0 || row >= a.rows) continue;
-            float x[8];
-            load8(kn + (size_t)row * a.ld_new, x);
-            for (int e = 0; e < 8; ++e) mk = fmaxf(mk, finite_abs(x[e]));
-            load8(vn + (size_t)row * a.ld_new, x);
-            for (int e = 0; e < 8; ++e) mv = fmaxf(mv, finite_abs(x[e]));
+        for (int pass = 0; pass < passes; ++pass) {
+            load(pass);
+            mk = fmaxf(mk, x.largest());
+            mv = fmaxf(mv, y.largest());
         }
         mk = wave_max(mk);
         mv = wave_max(mv);
@@ -276,35 +323,31 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
                     for (int q = 0; t + q < off; ++q) p[q] = (uint8_t)(w >> (8 * q));
             }
         }
+        __syncthreads();   // that dword is read before the new codes are written; s_max is free again
         const float ik = 1.f / sk, iv = 1.f / sv;   // powers of two: exact
-        for (int j = r0; j < run; j += kRowsPass) {
-            const int row = a.source != nullptr ? a.source[i + j] : i + j;
-            const bool real = row >= 0 && row < a.rows;
-            float x[8] = {}, y[8] = {};
-            if (real) {
-                load8(kn + (size_t)row * a.ld_new, x);
-                load8(vn + (size_t)row * a.ld_new, y);
+        for (int pass = 0; pass < passes; ++pass) {
+            if (passes > 1) load(pass);   // one pass's are still there
+            const int o = 4 * (q0 + pass * kQuads + tid / kChunks);
+            const int lo = max(off - o, 0), hi = min(off + run - o, 4);   // the quad's tokens of the run
+            if (lo >= hi) continue;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (t >= lo && t < hi) {
+                    uint2 w;
+                    w.x = e4m3_quad(x.at(t, 0) * ik, x.at(t, 1) * ik, x.at(t, 2) * ik, x.at(t, 3) * ik);
+                    w.y = e4m3_quad(x.at(t, 4) * ik, x.at(t, 5) * ik, x.at(t, 6) * ik, x.at(t, 7) * ik);
+                    *reinterpret_cast<uint2*>(kc + (size_t)(o + t) * D + c8) = w;
+                }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t w = e4m3_quad(y.at(0, e) * iv, y.at(1, e) * iv, y.at(2, e) * iv, y.at(3, e) * iv);
+                uint8_t* p = vc + (size_t)(c8 + e) * a.page + o;
+                if (lo == 0 && hi == 4) *reinterpret_cast<uint32_t*>(p) = w;
+                else
+                    for (int t = lo; t < hi; ++t) p[t] = (uint8_t)(w >> (8 * t));
             }
-            uint32_t* kd = reinterpret_cast<uint32_t*>(kc + (size_t)(off + j) * D + c8);
-            kd[0] = e4m3_quad(x[0] * ik, x[1] * ik, x[2] * ik, x[3] * ik);
-            kd[1] = e4m3_quad(x[4] * ik, x[5] * ik, x[6] * ik, x[7] * ik);
-            const uint32_t lo = e4m3_quad(y[0] * iv, y[1] * iv, y[2] * iv, y[3] * iv);
-            const uint32_t hi = e4m3_quad(y[4] * iv, y[5] * iv, y[6] * iv, y[7] * iv);
-            for (int e = 0; e < 8; ++e) turned[(c8 + e) * kPitch + off + j] = (uint8_t)((e < 4 ? lo : hi) >> (8 * (e & 3)));
-        }
-        __syncthreads();
-        const int q0 = off / 4, quads = (off + run + 3) / 4 - q0;
-        for (int e = tid; e < D * quads; e += kAppendThreads) {
-            const int d = e / quads, t = (q0 + e - d * quads) * 4;
-            const uint8_t* from = turned + d * kPitch + t;
-            uint8_t* p = vc + (size_t)d * a.page + t;
-            if (t >= off && t + 4 <= off + run) *reinterpret_cast<uint32_t*>(p) = *reinterpret_cast<const uint32_t*>(from);
-            else
-                for (int q = 0; q < 4; ++q)
-                    if (t + q >= off && t + q < off + run) p[q] = from[q];
         }
         if (tid == 0) a.k_scale[head] = sk, a.v_scale[head] = sv;
-        __syncthreads();   // `turned` and s_max are free again
     }
 }
 
