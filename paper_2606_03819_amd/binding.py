@@ -812,3 +812,87 @@ class Drafter2Prev(Drafter):
         if context is not None:
             self.context = context
         return super().step(h, root, weights)
+
+
+class PagedCache:
+    """The 8-bit cache of every layer of a verifier, and the pages of its sequences.
+
+    Pages, lengths and slots are shared by the layers and live on the GPU; a
+    step needs no host synchronisation and allocates nothing, so it can be
+    captured into a graph.  One decoding step of trees of n - 1 nodes:
+
+        for each layer: cache.attend(layer, q, k, v, mask, scale)
+        target, _ = treeflash_sample(logits, uniform, ...)
+        walk = treeflash_accept(tree, target, cache.gamma)
+        cache.advance(walk)
+        for each layer: cache.append(layer, k, v)
+
+    A prompt is added with cache.extend(add_len, max_tokens) and then append for
+    each layer.  `status` reads 0 where the last advance or extend found the
+    pages it needed; otherwise nothing was taken and append writes nothing."""
+
+    def __init__(self, layers: int, b: int, n: int, gamma: int, Hq: int, Hkv: int, D: int, num_pages: int, max_pages: int,
+                 page_size: int = 64, dtype: torch.dtype = torch.bfloat16, device="cuda"):
+        dev = torch.empty((0,), device=device).device
+        self.dev, self.layers, self.b, self.n, self.gamma = dev, layers, b, n, gamma
+        self.Hq, self.Hkv, self.D, self.page_size, self.dtype = Hq, Hkv, D, page_size, dtype
+        nbytes = treeflash_tree_attention_workspace_bytes(b, n, Hq, Hkv, D, page_size, max_pages, dtype)
+        if nbytes == 0:
+            raise ValueError("invalid cache shapes")
+        self.workspace = alloc_workspace(nbytes, dev)
+        i32 = dict(dtype=torch.int32, device=dev)
+        u8 = dict(dtype=torch.uint8, device=dev)
+        self.k = [torch.zeros((num_pages, Hkv, page_size, D), **u8).view(E4M3) for _ in range(layers)]
+        self.v = [torch.zeros((num_pages, Hkv, D, page_size), **u8).view(E4M3) for _ in range(layers)]
+        self.k_scale = [torch.ones((num_pages, Hkv), dtype=torch.float32, device=dev) for _ in range(layers)]
+        self.v_scale = [torch.ones((num_pages, Hkv), dtype=torch.float32, device=dev) for _ in range(layers)]
+        self.block_table = torch.zeros((b, max_pages), **i32)
+        self.free_pages = torch.arange(num_pages - 1, -1, -1, **i32)   # page 0 is taken first
+        self.context_len = torch.zeros((b,), **i32)
+        self.free_count = torch.full((1,), num_pages, **i32)
+        self._step_lists = self._lists(b * (gamma + 1))
+        self.slots = self._step_lists   # of the last advance or extend
+        self.out = torch.empty((b, n, Hq, D), dtype=dtype, device=dev)
+        self.lse = torch.empty((b, n, Hq), dtype=torch.float32, device=dev)
+
+    def _lists(self, max_tokens: int) -> dict:
+        e = dict(dtype=torch.int32, device=self.dev)
+        return {"context_len": self.context_len, "free_count": self.free_count,
+                "start": torch.empty((self.b + 1,), **e), "page_start": torch.empty((self.b + 1,), **e),
+                "slot": torch.empty((max_tokens,), **e), "position": torch.empty((max_tokens,), **e),
+                "source": torch.empty((max_tokens,), **e), "status": torch.empty((1,), **e)}
+
+    @property
+    def status(self) -> torch.Tensor:
+        return self.slots["status"]
+
+    def attend(self, layer: int, q, k_new, v_new, mask, scale: float, new_len=None, out=None, lse=None):
+        """Attention of the tree's positions in one layer, into `out` and `lse` (held buffers if not given,
+        which the next call overwrites)."""
+        return treeflash_tree_attention(q, k_new, v_new, mask, self.context_len, self.block_table, self.k[layer],
+                                        self.v[layer], self.k_scale[layer], self.v_scale[layer], scale, new_len,
+                                        self.workspace, self.out if out is None else out, self.lse if lse is None else lse)
+
+    def advance(self, walk: Dict[str, torch.Tensor]) -> dict:
+        """Pages and slots of the root and the accepted nodes of treeflash_accept's result."""
+        self.slots = self._step_lists
+        return treeflash_cache_slots(self.context_len, walk["accept_len"], self.free_pages, self.free_count,
+                                     self.block_table, self.page_size, self.b * (self.gamma + 1),
+                                     accepted=walk["accepted"], n=self.n, out=self.slots)
+
+    def extend(self, add_len: torch.Tensor, max_tokens: int, n: int = 0) -> dict:
+        """Pages and slots of add_len [b] further tokens, max_tokens at most together: rows of packed keys and
+        values (n 0), or of n for each sequence.  Allocates its lists."""
+        self.slots = self._lists(max_tokens)
+        return treeflash_cache_slots(self.context_len, add_len, self.free_pages, self.free_count, self.block_table,
+                                     self.page_size, max_tokens, n=n, out=self.slots)
+
+    def append(self, layer: int, k_new, v_new):
+        """Keys and values of the last advance or extend, in one layer."""
+        treeflash_cache_append(k_new, v_new, self.slots["slot"], self.k[layer], self.v[layer], self.k_scale[layer],
+                               self.v_scale[layer], source=self.slots["source"])
+
+    def release(self, done: torch.Tensor):
+        """Gives back the pages of the sequences with done [b] (uint8)."""
+        treeflash_cache_release(done, self.context_len, self.block_table, self.free_pages, self.free_count,
+                                self.page_size)

@@ -10,6 +10,7 @@ namespace tf {
 constexpr int kPlanThreads = 1024;
 constexpr int kFillThreads = 256;
 constexpr int kFillPer = 4;            // tokens a thread of the fill places
+constexpr int kFillSeqs = 2048;        // sequences whose offsets it keeps in LDS
 // Tokens up to which the planning workgroup fills the lists itself, which
 // saves the second launch.
 constexpr int kFillAlone = 1 << 14;
@@ -164,9 +165,18 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(SlotsArgs a, i
     }
 }
 
+// The search for a token's sequence goes through LDS where the offsets fit.
 __global__ __launch_bounds__(kFillThreads) void cache_fill_kernel(SlotsArgs a) {
+    __shared__ int32_t start[kFillSeqs + 1], page_start[kFillSeqs + 1];
     const int i0 = blockIdx.x * (kFillThreads * kFillPer);
-    fill_slots(a, a.start, a.page_start, i0 + threadIdx.x, min(i0 + kFillThreads * kFillPer, a.max_tokens), kFillThreads);
+    const int i1 = min(i0 + kFillThreads * kFillPer, a.max_tokens);
+    if (a.b <= kFillSeqs) {
+        for (int s = threadIdx.x; s <= a.b; s += kFillThreads) start[s] = a.start[s], page_start[s] = a.page_start[s];
+        __syncthreads();
+        fill_slots(a, start, page_start, i0 + threadIdx.x, i1, kFillThreads);
+    } else {
+        fill_slots(a, a.start, a.page_start, i0 + threadIdx.x, i1, kFillThreads);
+    }
 }
 
 // One workgroup: the finished sequences' pages go onto the stack in order.
@@ -236,36 +246,45 @@ struct TokenQuad {
     }
 };
 
-// Workgroup (`per` tokens of the list, head): for each run that begins among
-// its tokens, the run's largest values, the scale, what the page held rounded
-// again where the scale rose, the new codes.  The page's first token of the
-// list leads its run, so every page and head has one writer and no atomics.
-// A thread takes four tokens' eight dimensions (tokens 4q..4q+3 of the page),
-// all loads in flight at once: four conversions then give a dword along the
-// dimensions for the keys, and one along the tokens for the values' [D, page]
-// side, without a turn through LDS.  Bound by memory latency up to a few
-// pages a CU, by the reads and writes beyond.
+// Workgroup (`per` tokens of the list, head, keys or values): for each run that
+// begins among its tokens, the run's largest value, the scale, what the page
+// held rounded again where the scale rose, the new codes.  The page's first
+// token of the list leads its run, so every page and head has one writer and
+// no atomics.  A thread takes four tokens' eight dimensions (tokens 4q..4q+3 of
+// the page), all loads in flight at once: four conversions then give a dword
+// along the dimensions for the keys, or along the tokens for the values' [D,
+// page] side, which goes through LDS so that a store holds 16 tokens.  What
+// bounds it is a chain of three loads (slot, source, row), so how many
+// workgroups a CU holds: keys and values apart and at most 64 registers give
+// eight (27 thousand tokens of 8 heads in pages of 64: 70 us together at four a
+// CU, 44 so).
 template <class T, int D>
-__global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs a, int per) {
+__global__ __launch_bounds__(kAppendThreads, sizeof(T) == 2 ? 8 : 6) void cache_append_kernel(AppendArgs a, int per) {
     constexpr int kChunks = D / 8;                        // threads across a row
     constexpr int kQuads = kAppendThreads / kChunks;      // quads of tokens a pass
-    __shared__ float s_max[2][kAppendThreads / 64];
+    constexpr int kPitch = 128 / 4 + 1;
+    __shared__ float s_max[kAppendThreads / 64];
+    __shared__ uint32_t turned[D * kPitch];               // values: four tokens' codes a dword
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int h = blockIdx.y;
-    const int end = (int)min((long long)a.N, (long long)(blockIdx.x + 1) * per);
+    // keys and values and the heads of the same tokens follow one another on an
+    // XCD: their pieces of a row and of the lists come from its L2
+    const int y = blockIdx.x / 8, unit = y % (2 * a.Hkv);
+    const int block = y / (2 * a.Hkv) * 8 + blockIdx.x % 8, h = unit / 2;
+    const bool values = (unit & 1) != 0;                  // uniform
+    const int end = (int)min((long long)a.N, (long long)(block + 1) * per);
     const long long limit = (long long)a.num_pages * a.page;
     const int c8 = (tid % kChunks) * 8;
-    const T* kn = static_cast<const T*>(a.k_new) + (size_t)h * D + c8;
-    const T* vn = static_cast<const T*>(a.v_new) + (size_t)h * D + c8;
+    const T* rows = static_cast<const T*>(values ? a.v_new : a.k_new) + (size_t)h * D + c8;
+    float* scale = values ? a.v_scale : a.k_scale;
     // the tokens that lead a run, all looked at at once (per <= 64)
-    const int mine = (int)blockIdx.x * per + lane;
+    const int mine = block * per + lane;
     bool leads = false;
     if (lane < per && mine < end) {
         const int sl = a.slot[mine], before = mine > 0 ? a.slot[mine - 1] : -1;
         leads = sl >= 0 && sl < limit && ((sl & (a.page - 1)) == 0 || before != sl - 1);
     }
     for (unsigned long long todo = __ballot(leads); todo != 0; todo &= todo - 1) {   // uniform over the workgroup
-        const int i = (int)blockIdx.x * per + __builtin_ctzll(todo);
+        const int i = block * per + __builtin_ctzll(todo);
         const int sl = a.slot[i];
         const int off = sl & (a.page - 1), id = sl / a.page;
         const int most = min(a.page - off, a.N - i);
@@ -274,7 +293,7 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
         const int run = ~b0 != 0 ? __builtin_ctzll(~b0) : (~b1 != 0 ? 64 + __builtin_ctzll(~b1) : 128);
 
         const int q0 = off / 4, passes = ((off + run + 3) / 4 - q0 + kQuads - 1) / kQuads;
-        TokenQuad<T> x, y;
+        TokenQuad<T> x;
         auto load = [&](int pass) {
             const int o = 4 * (q0 + pass * kQuads + tid / kChunks) - off;   // the quad's first token, in the run
             int row[4];
@@ -284,70 +303,76 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
                 if (o + t >= 0 && o + t < run) row[t] = a.source != nullptr ? a.source[i + o + t] : i + o + t;
                 if (row[t] >= a.rows) row[t] = -1;
             }
-            x.load(kn, a.ld_new, row);
-            y.load(vn, a.ld_new, row);
+            x.load(rows, a.ld_new, row);
         };
-        float mk = 0.f, mv = 0.f;
+        float most_abs = 0.f;
         for (int pass = 0; pass < passes; ++pass) {
             load(pass);
-            mk = fmaxf(mk, x.largest());
-            mv = fmaxf(mv, y.largest());
+            most_abs = fmaxf(most_abs, x.largest());
         }
-        mk = wave_max(mk);
-        mv = wave_max(mv);
-        if (lane == 0) s_max[0][wave] = mk, s_max[1][wave] = mv;
+        most_abs = wave_max(most_abs);
+        if (lane == 0) s_max[wave] = most_abs;
         __syncthreads();
-        for (int w = 0; w < kAppendThreads / 64; ++w) {
-            mk = fmaxf(mk, s_max[0][w]);
-            mv = fmaxf(mv, s_max[1][w]);
-        }
+        for (int w = 0; w < kAppendThreads / 64; ++w) most_abs = fmaxf(most_abs, s_max[w]);
         const size_t head = (size_t)id * a.Hkv + h;
-        float sk = pow2_scale(mk), sv = pow2_scale(mv);
-        const float ok = off > 0 ? a.k_scale[head] : 0.f, ov = off > 0 ? a.v_scale[head] : 0.f;
-        sk = fmaxf(sk, ok);
-        sv = fmaxf(sv, ov);
-        uint8_t* kc = static_cast<uint8_t*>(a.k_cache) + head * a.page * D;
-        uint8_t* vc = static_cast<uint8_t*>(a.v_cache) + head * a.page * D;
-        if (off > 0 && sk != ok) {
-            uint32_t* p = reinterpret_cast<uint32_t*>(kc);
-            for (int e = tid; e < off * (D / 4); e += kAppendThreads) p[e] = e4m3_rescale(p[e], ok / sk);
-        }
-        if (off > 0 && sv != ov) {
-            const int quads = (off + 3) / 4;
-            for (int e = tid; e < D * quads; e += kAppendThreads) {
-                const int d = e / quads, t = (e - d * quads) * 4;
-                uint8_t* p = vc + (size_t)d * a.page + t;
-                const uint32_t w = e4m3_rescale(*reinterpret_cast<const uint32_t*>(p), ov / sv);
-                if (t + 4 <= off) *reinterpret_cast<uint32_t*>(p) = w;
-                else   // the dword that the run goes on in
-                    for (int q = 0; t + q < off; ++q) p[q] = (uint8_t)(w >> (8 * q));
+        const float old = off > 0 ? scale[head] : 0.f;
+        const float now = fmaxf(pow2_scale(most_abs), old);
+        uint8_t* cache = static_cast<uint8_t*>(values ? a.v_cache : a.k_cache) + head * a.page * D;
+        if (off > 0 && now != old) {
+            if (!values) {
+                uint32_t* p = reinterpret_cast<uint32_t*>(cache);
+                for (int e = tid; e < off * (D / 4); e += kAppendThreads) p[e] = e4m3_rescale(p[e], old / now);
+            } else {
+                const int quads = (off + 3) / 4;
+                for (int e = tid; e < D * quads; e += kAppendThreads) {
+                    const int d = e / quads, t = (e - d * quads) * 4;
+                    uint8_t* p = cache + (size_t)d * a.page + t;
+                    const uint32_t w = e4m3_rescale(*reinterpret_cast<const uint32_t*>(p), old / now);
+                    if (t + 4 <= off) *reinterpret_cast<uint32_t*>(p) = w;
+                    else   // the dword that the run goes on in
+                        for (int q = 0; t + q < off; ++q) p[q] = (uint8_t)(w >> (8 * q));
+                }
             }
         }
         __syncthreads();   // that dword is read before the new codes are written; s_max is free again
-        const float ik = 1.f / sk, iv = 1.f / sv;   // powers of two: exact
+        const float f = 1.f / now;   // a power of two: exact
         for (int pass = 0; pass < passes; ++pass) {
             if (passes > 1) load(pass);   // one pass's are still there
             const int o = 4 * (q0 + pass * kQuads + tid / kChunks);
             const int lo = max(off - o, 0), hi = min(off + run - o, 4);   // the quad's tokens of the run
             if (lo >= hi) continue;
+            if (!values) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if (t >= lo && t < hi) {
-                    uint2 w;
-                    w.x = e4m3_quad(x.at(t, 0) * ik, x.at(t, 1) * ik, x.at(t, 2) * ik, x.at(t, 3) * ik);
-                    w.y = e4m3_quad(x.at(t, 4) * ik, x.at(t, 5) * ik, x.at(t, 6) * ik, x.at(t, 7) * ik);
-                    *reinterpret_cast<uint2*>(kc + (size_t)(o + t) * D + c8) = w;
-                }
+                for (int t = 0; t < 4; ++t)
+                    if (t >= lo && t < hi) {
+                        uint2 w;
+                        w.x = e4m3_quad(x.at(t, 0) * f, x.at(t, 1) * f, x.at(t, 2) * f, x.at(t, 3) * f);
+                        w.y = e4m3_quad(x.at(t, 4) * f, x.at(t, 5) * f, x.at(t, 6) * f, x.at(t, 7) * f);
+                        *reinterpret_cast<uint2*>(cache + (size_t)(o + t) * D + c8) = w;
+                    }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t w = e4m3_quad(y.at(0, e) * iv, y.at(1, e) * iv, y.at(2, e) * iv, y.at(3, e) * iv);
-                uint8_t* p = vc + (size_t)(c8 + e) * a.page + o;
-                if (lo == 0 && hi == 4) *reinterpret_cast<uint32_t*>(p) = w;
-                else
-                    for (int t = lo; t < hi; ++t) p[t] = (uint8_t)(w >> (8 * t));
+                for (int e = 0; e < 8; ++e)
+                    turned[(c8 + e) * kPitch + o / 4] = e4m3_quad(x.at(0, e) * f, x.at(1, e) * f, x.at(2, e) * f, x.at(3, e) * f);
             }
         }
-        if (tid == 0) a.k_scale[head] = sk, a.v_scale[head] = sv;
+        if (values) {   // a dimension's tokens lie together: 16 of them a store
+            __syncthreads();
+            const int g0 = off / 16, groups = (off + run + 15) / 16 - g0;
+            for (int e = tid; e < D * groups; e += kAppendThreads) {
+                const int d = e / groups, o = (g0 + e - d * groups) * 16;
+                const uint32_t* from = turned + d * kPitch + o / 4;
+                uint8_t* p = cache + (size_t)d * a.page + o;
+                if (o >= off && o + 16 <= off + run) {
+                    *reinterpret_cast<u32x4*>(p) = u32x4{from[0], from[1], from[2], from[3]};
+                } else {
+                    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(from);
+                    for (int t = max(off - o, 0); t < min(off + run - o, 16); ++t) p[t] = bytes[t];
+                }
+            }
+            __syncthreads();   // `turned` is free again
+        }
+        if (tid == 0) scale[head] = now;
     }
 }
 
@@ -367,10 +392,14 @@ hipError_t launch_cache_release(const ReleaseArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_cache_append(const AppendArgs& a, int D, bool bf16, hipStream_t stream) {
-    // about 8192 workgroups: single tokens get one each, long lists share one among up to a page
+    // single tokens get a workgroup each while there are few, long lists one for
+    // up to 64 tokens (27 thousand tokens of 8 heads: 58 us by 32, 44 by 64,
+    // where fewer workgroups find no run of their own)
     int per = 1;
-    while (per < 64 && (long long)a.N * a.Hkv > 8192ll * per) per *= 2;
-    const dim3 grid((unsigned)((a.N - 1) / per + 1), (unsigned)a.Hkv);
+    while (per < 64 && (long long)a.N * a.Hkv > 4096ll * per) per *= 2;
+    const long long blocks = (((long long)a.N - 1) / per / 8 + 1) * 8;
+    if (blocks * a.Hkv * 2 > 0x7fffffffll) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(blocks * a.Hkv * 2));
     if (bf16 && D == 128)
         hipLaunchKernelGGL((cache_append_kernel<uint16_t, 128>), grid, dim3(kAppendThreads), 0, stream, a, per);
     else if (bf16)

@@ -545,6 +545,65 @@ def test_a_replayed_graph_of_the_step():
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
 
 
+def test_paged_cache_of_two_layers():
+    """Prompts, two decoding steps, a release and a new prompt through PagedCache, each layer against the oracle."""
+    rng = np.random.default_rng(30)
+    b, n, gamma, Hq, H, D, page, layers = 3, 9, 4, 4, 2, 64, 16, 2
+    pc = binding.PagedCache(layers, b, n, gamma, Hq, H, D, num_pages=40, max_pages=12, page_size=page)
+    ref = [cache_np(dict(k_cache=pc.k[i], v_cache=pc.v[i], k_scale=pc.k_scale[i], v_scale=pc.v_scale[i])) for i in range(layers)]
+    state = dict(ctx=[0] * b, table=pc.block_table.cpu().numpy(), count=40)
+
+    def plan(add, acc, n_rows, max_tokens):
+        w = oracle.cache_slots(state["ctx"], add, acc, pc.free_pages.tolist(), state["count"], state["table"], n_rows, page, max_tokens)
+        assert w["status"] == int(pc.status) == 0
+        state.update(ctx=w["context_len"].tolist(), table=w["block_table"], count=w["free_count"])
+        assert pc.context_len.tolist() == state["ctx"] and int(pc.free_count) == state["count"]
+        assert np.array_equal(pc.block_table.cpu().numpy(), state["table"])
+        return w
+
+    def put(k, v, w):
+        for i in range(layers):
+            pc.append(i, k * (i + 1), v * (i + 1))
+            ref[i] = oracle.cache_append(f64(k * (i + 1)).reshape(-1, H, D), f64(v * (i + 1)).reshape(-1, H, D), w["slot"],
+                                         w["source"], *ref[i])
+            got = cache_np(dict(k_cache=pc.k[i], v_cache=pc.v[i], k_scale=pc.k_scale[i], v_scale=pc.v_scale[i]))
+            assert all(np.array_equal(x, y) for x, y in zip(got, ref[i]))
+
+    def prompt(add):
+        kv = torch.tensor(rng.standard_normal((sum(add), 2 * H, D))).to(torch.bfloat16).cuda()
+        pc.extend(i32(add), sum(add) + 2)
+        put(kv[:, :H], kv[:, H:], plan(add, None, 0, sum(add) + 2))
+
+    prompt([37, 5, 70])
+    for step in range(3):
+        qkv = torch.tensor(rng.standard_normal((b, n, Hq + 2 * H, D))).to(torch.bfloat16).cuda()
+        q, k, v = qkv[:, :, :Hq], qkv[:, :, Hq:Hq + H], qkv[:, :, Hq + H:]
+        mask = torch.tensor(tree_masks(rng, b, n)).cuda()
+        for i in range(layers):
+            out, lse = pc.attend(i, q, k, v, mask, 0.1)
+            cache = dict(k_cache=pc.k[i], v_cache=pc.v[i], k_scale=pc.k_scale[i], v_scale=pc.v_scale[i])
+            check_attention(out, lse, q, k, v, mask, state["ctx"], pc.block_table, cache, 0.1)
+        ln = rng.integers(0, gamma + 1, b)
+        acc = np.where(np.arange(gamma) < ln[:, None], np.sort(rng.permutation(n - 1)[:gamma]), -1).astype(np.int32)
+        acc = np.broadcast_to(acc, (b, gamma)).copy()
+        pc.advance(dict(accept_len=i32(ln), accepted=i32(acc)))
+        put(k, v, plan(ln, acc, n, b * (gamma + 1)))
+        if step == 1:
+            held = -(-state["ctx"][1] // page)
+            pc.release(torch.tensor([0, 1, 0], dtype=torch.uint8).cuda())
+            state["ctx"][1] = 0
+            state["count"] += held
+            assert int(pc.free_count) == state["count"]
+            prompt([0, 20, 0])
+    pc.extend(i32([1000, 0, 0]), 2000)      # more than the table holds: nothing happens
+    assert int(pc.status) == 3 and pc.context_len.tolist() == state["ctx"]
+    before = [x.view(torch.uint8).clone() for x in (*pc.k, *pc.v)]
+    pc.append(0, k, v)
+    assert all(torch.equal(x.view(torch.uint8), y) for x, y in zip((*pc.k, *pc.v), before))
+    with pytest.raises(ValueError):
+        binding.PagedCache(1, 1, 1, 1, 4, 2, 80, 4, 4)
+
+
 def test_calls_on_two_streams_at_once():
     rng = np.random.default_rng(18)
     z = [likely(rng, 4, 5, 20000, torch.bfloat16) for _ in range(2)]
