@@ -222,10 +222,9 @@ int most_splits(long long groups, int slots, int max_pages, int page) {
 int row_blocks(int Hq, int Hkv) { return (Hq / Hkv + kGroupRows - 1) / kGroupRows; }
 
 int splits_of(int b, int n, int Hq, int Hkv, int page, int max_pages, bool bf16) {
-    // workgroups on 256 CUs: four where a wave keeps one row tile or fp32 sums, two where it keeps more
-    if (!bf16) return most_splits((long long)b * n * Hkv * row_blocks(Hq, Hkv), 1024, max_pages, page);
-    const TileBlocks tb = tile_blocks(n, Hq, Hkv);
-    return most_splits((long long)b * Hkv * tb.blocks, tb.tiles == 1 ? 1024 : 512, max_pages, page);
+    // workgroups on 256 CUs: two by the matrix kernel's registers, four of the row kernel
+    if (bf16) return most_splits((long long)b * Hkv * tile_blocks(n, Hq, Hkv).blocks, 512, max_pages, page);
+    return most_splits((long long)b * n * Hkv * row_blocks(Hq, Hkv), 1024, max_pages, page);
 }
 
 template <class T>

@@ -20,9 +20,11 @@
 // kSlack, since raising it means scaling all of O^T and a maximum over the
 // lanes that share a row.
 //
-// What bounds it: with many rows the vector units, which turn 64 codes a lane
-// and a tile into operands (shared by the NQ row tiles) and take 8 exponents
-// a row tile; with few rows the reads.
+// What bounds it: with few rows the reads (64 sequences' single tokens over up
+// to 8192: 152 us, 5.2 TB/s of cache); with many the chain through a tile at
+// two waves a SIMD -- 64 codes a lane turned into operands, shared by the NQ row
+// tiles, then 8 exponents a row tile (16 sequences, 33 positions of 4 heads a
+// key head, up to 16384 tokens: 200 us, 0.55 PFLOP/s; without any loads 187).
 #include "attend.hpp"
 
 namespace tf {
@@ -66,11 +68,11 @@ __device__ __forceinline__ uint32_t f16_pair(float a, float b) {
 template <int PAGE>
 struct TilePages {
     int id[PAGE == 16 ? 2 : 1];
-    __device__ void load(const AttendArgs& a, const int32_t* table, int t0, int step) {
+    __device__ void load(const AttendArgs& a, const int32_t* table, int t0, int kStep) {
         const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int h = 0; h < (PAGE == 16 ? 2 : 1); ++h) {
-            const long long t = (long long)t0 + (long long)lane * step + 16 * h;
+            const long long t = (long long)t0 + (long long)lane * kStep + 16 * h;
             const int p = table[min((int)(t / PAGE), a.max_pages - 1)];
             id[h] = p >= 0 && p < a.num_pages ? p : -1;
         }
@@ -223,54 +225,56 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
     const int lane_k = (kt & (PAGE - 1)) * D + 16 * quarter;
     const int lane_v = col * PAGE + (8 * quarter & (PAGE - 1));
     int t0 = lo + wave * 32;
-    // keys are read again as soon as their products are made, values likewise,
-    // so that one set of registers each is in flight through the other's work
-    u32x4 k[2][kC];
-    uint2 v[kT];
-    float ks_next = 0.f, vs_next = 0.f;
-    TilePlace<PAGE> next;
+    // The next tile's keys and values are in flight through the work on this one;
+    // with three row tiles there are registers for one set alone, and each is
+    // read again as soon as it has been used.
+    constexpr bool kOneSet = NQ == kMostTiles;
+    struct Tile {
+        u32x4 k[2][kC];
+        uint2 v[kT];
+        float ks, vs;
+        TilePlace<PAGE> place;
+    } even, odd;
     TilePages<PAGE> pages, later;   // of tiles 64i.. and 64(i+1)..
-    if (t0 < hi) {
-        pages.load(a, table, t0, kStep);
-        later = pages;
-        next.set(a, pages, 0, hk, t0, hi);
-        load_keys<D, PAGE>(k, a, next, lane_k);
-        ks_next = scale_of<PAGE>(a.k_scale, next);
-        vs_next = scale_of<PAGE>(a.v_scale, next);
-        load_values<D, PAGE>(v, a, next, lane_v);
-    }
-    for (int nth = 0; t0 < hi; t0 += kStep, ++nth) {
-        const TilePlace<PAGE> here = next;
-        const float k_scale = ks_next, v_scale = vs_next;
+    int nth = 0;
+    auto work = [&](Tile& t, Tile& next) {
+        const TilePlace<PAGE> place = t.place;
+        const float k_scale = t.ks, v_scale = t.vs;
         const bool more = t0 + kStep < hi;
+        TilePlace<PAGE> to = place;
         if (more) {
             if ((nth & 63) == 0) later.load(a, table, (int)min((long long)t0 + 64 * kStep, (long long)hi - 1), kStep);   // used 63 tiles on
             if ((nth & 63) == 63) pages = later;
-            next.set(a, pages, (nth + 1) & 63, hk, t0 + kStep, hi);
+            ++nth;
+            to.set(a, pages, nth & 63, hk, t0 + kStep, hi);
+            if (!kOneSet) {
+                load_keys<D, PAGE>(next.k, a, to, lane_k);
+                load_values<D, PAGE>(next.v, a, to, lane_v);
+            }
+            next.ks = scale_of<PAGE>(a.k_scale, to);
+            next.vs = scale_of<PAGE>(a.v_scale, to);
         }
         f32x4 acc[NQ][2];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) acc[n][0] = acc[n][1] = f32x4{};
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int c = 0; c < kC; ++c)
 #pragma unroll
-            for (int c = 0; c < kC; ++c) {
-                const u32x4 k0 = codes_bf16(k[h][c][0], k[h][c][1]), k1 = codes_bf16(k[h][c][2], k[h][c][3]);
+            for (int d = 0; d < 2; ++d) {
+                const u32x4 k0 = codes_bf16(t.k[0][c][2 * d], t.k[0][c][2 * d + 1]);
+                const u32x4 k1 = codes_bf16(t.k[1][c][2 * d], t.k[1][c][2 * d + 1]);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) {
-                    acc[n][h] = mfma_bf16(k0, q[n][c][0], acc[n][h]);
-                    acc[n][h] = mfma_bf16(k1, q[n][c][1], acc[n][h]);
+                    acc[n][0] = mfma_bf16(k0, q[n][c][d], acc[n][0]);
+                    acc[n][1] = mfma_bf16(k1, q[n][c][d], acc[n][1]);
                 }
             }
-        if (more) {
-            load_keys<D, PAGE>(k, a, next, lane_k);
-            ks_next = scale_of<PAGE>(a.k_scale, next);
-            vs_next = scale_of<PAGE>(a.v_scale, next);
-        }
+        if (kOneSet && more) load_keys<D, PAGE>(next.k, a, to, lane_k);
+        __builtin_amdgcn_sched_barrier(0);   // the values' operands are made after the weights: else they spill
         const int e = (int)(__float_as_uint(v_scale) >> 23) - 127;
         const float ks = k_scale * qscale, inv = __uint_as_float((uint32_t)(127 - e) << 23);
-        const bool part = !here.whole();   // uniform
-        const int left = here.left(quarter);
+        const bool part = !place.whole();   // uniform
+        const int left = place.left(quarter);
         u32x4 p[NQ];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -292,15 +296,36 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
             const int l0 = min(left, 4), l1 = max(left - 4, 0);
             const uint32_t m0 = l0 == 4 ? ~0u : (1u << (8 * l0)) - 1u, m1 = l1 == 4 ? ~0u : (1u << (8 * l1)) - 1u;
 #pragma unroll
-            for (int c = 0; c < kT; ++c) v[c].x &= m0, v[c].y &= m1;
+            for (int c = 0; c < kT; ++c) t.v[c].x &= m0, t.v[c].y &= m1;
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < kT; ++c) {
-            const u32x4 x = codes_f16(v[c].x, v[c].y);
+            const u32x4 x = codes_f16(t.v[c].x, t.v[c].y);
 #pragma unroll
             for (int n = 0; n < NQ; ++n) o[n][c] = mfma_f16(x, p[n], o[n][c]);
         }
-        if (more) load_values<D, PAGE>(v, a, next, lane_v);
+        if (kOneSet && more) load_values<D, PAGE>(next.v, a, to, lane_v);
+        next.place = to;
+        t0 += kStep;
+    };
+    if (t0 < hi) {
+        pages.load(a, table, t0, kStep);
+        later = pages;
+        even.place.set(a, pages, 0, hk, t0, hi);
+        load_keys<D, PAGE>(even.k, a, even.place, lane_k);
+        load_values<D, PAGE>(even.v, a, even.place, lane_v);
+        even.ks = scale_of<PAGE>(a.k_scale, even.place);
+        even.vs = scale_of<PAGE>(a.v_scale, even.place);
+    }
+    while (t0 < hi) {
+        if constexpr (kOneSet) {
+            work(even, even);
+        } else {
+            work(even, odd);
+            if (t0 >= hi) break;
+            work(odd, even);
+        }
     }
 
     if (range == sp.count - 1) {
@@ -371,7 +396,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
                     *reinterpret_cast<const u32x4*>(vn + (size_t)min(j0 + r, nl - 1) * a.ld_new + d);
             }
             __builtin_amdgcn_wave_barrier();
-            bool odd = false;
+            bool strange = false;
 #pragma unroll
             for (int c = 0; c < kT; ++c) {
                 u32x4 v;
@@ -379,7 +404,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
                 for (int j = 0; j < 8; ++j) {
                     uint32_t x = turn[8 * quarter + j][16 * c + col];
                     const bool bad = (x & 0x7f80u) == 0x7f80u;
-                    odd |= bad;
+                    strange |= bad;
                     x = bad ? 0u : x;
                     if (j & 1) v[j >> 1] |= x << 16;
                     else v[j >> 1] = x;
@@ -391,7 +416,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
                 }
             }
             __builtin_amdgcn_wave_barrier();
-            if (__any(odd)) {
+            if (__any(strange)) {
                 float (&lw)[32][kTileRows] = shared[wave].weights;
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) {
