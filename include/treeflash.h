@@ -434,7 +434,8 @@ tf_status_t treeflash_cache_release(const uint8_t *done, const int32_t *context_
  * where it rises, the o tokens are rounded again.  Codes are rounded to nearest
  * even, infinities stored as +-448 and NaN as NaN, neither entering the scale.
  * Bytes of a page behind the run stay as they were.  Two runs of one list in
- * the same page give unspecified values. */
+ * the same page give unspecified values.  N*Hkv <= 2^28, else
+ * TF_ERR_UNSUPPORTED. */
 tf_status_t treeflash_cache_append(const void *k_new, const void *v_new, long long ld_new, int rows,
                                    const int32_t *slot, const int32_t *source, int N, int Hkv, int D,
                                    int page_size, int num_pages, tf_dtype_t dt, void *k_cache, void *v_cache,
@@ -467,7 +468,8 @@ size_t treeflash_tree_attention_workspace_bytes(int b, int n, int Hq, int Hkv, i
  * aligned, ld_q and ld_new times the element size multiples of 16.
  * bf16 multiplies bf16 queries with the stored codes and fp16 softmax weights
  * with the cached values (both exact in their 8-bit operand), sums in fp32;
- * TF_F32 works in fp32 throughout.  n <= 4096. */
+ * TF_F32 works in fp32 throughout.  n <= 4096; b*n*Hq <= 2^23, else
+ * TF_ERR_UNSUPPORTED. */
 tf_status_t treeflash_tree_attention(const void *q, long long ld_q, const void *k_new, const void *v_new,
                                      long long ld_new, const uint8_t *mask, const int32_t *new_len,
                                      const int32_t *context_len, const int32_t *block_table,

@@ -13,6 +13,8 @@ using namespace tf;
 
 constexpr long long kMaxPositions = 1 << 20;   // b * n
 constexpr int kMaxVocab = 1 << 22;
+constexpr long long kMaxQueryRows = 1 << 23;   // b * n * Hq: a launch's threads stay below 2^32
+constexpr long long kMaxHeadTokens = 1 << 28;  // N * Hkv of an append, likewise
 
 bool opt4(const void* p) { return p == nullptr || aligned4(p); }
 
@@ -39,8 +41,9 @@ tf_status_t attend_shapes(int b, int n, int Hq, int Hkv, int D, int page_size, i
     if (!dtype_ok(dt) || b < 1 || n < 1 || n > 4096 || (long long)b * n > kMaxPositions) return TF_ERR_INVALID_ARG;
     if (Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq > 4096) return TF_ERR_INVALID_ARG;
     tf_status_t st = head_status(Hkv, D);
-    if (st != TF_OK) return st;
-    return page_status(page_size, max_pages);
+    if (st == TF_OK) st = page_status(page_size, max_pages);
+    if (st == TF_OK && (long long)b * n * Hq > kMaxQueryRows) st = TF_ERR_UNSUPPORTED;
+    return st;
 }
 
 }  // namespace
@@ -116,6 +119,7 @@ tf_status_t treeflash_cache_append(const void* k_new, const void* v_new, long lo
     tf_status_t st = head_status(Hkv, D);
     if (st != TF_OK) return st;
     if ((st = page_status(page_size, num_pages)) != TF_OK) return st;
+    if ((long long)N * Hkv > kMaxHeadTokens) return TF_ERR_UNSUPPORTED;
     if ((st = row_status(ld_new, (long long)Hkv * D, dt)) != TF_OK) return st;
     if ((st = vec_status_all({k_new, v_new}, dt)) != TF_OK) return st;
     if (!aligned16(k_cache) || !aligned16(v_cache)) return TF_ERR_UNSUPPORTED;

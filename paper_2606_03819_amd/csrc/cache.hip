@@ -398,7 +398,6 @@ hipError_t launch_cache_append(const AppendArgs& a, int D, bool bf16, hipStream_
     int per = 1;
     while (per < 64 && (long long)a.N * a.Hkv > 4096ll * per) per *= 2;
     const long long blocks = (((long long)a.N - 1) / per / 8 + 1) * 8;
-    if (blocks * a.Hkv * 2 > 0x7fffffffll) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(blocks * a.Hkv * 2));
     if (bf16 && D == 128)
         hipLaunchKernelGGL((cache_append_kernel<uint16_t, 128>), grid, dim3(kAppendThreads), 0, stream, a, per);

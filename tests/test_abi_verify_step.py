@@ -80,7 +80,7 @@ APPEND = dict(k=P, v=P, ld=1024, rows=5, slot=P, src=None, N=5, H=8, D=128, page
                             (dict(pages=0), INVALID), (dict(pages=1 << 26), INVALID), (dict(ld=1023), INVALID),
                             (dict(ld=1028), UNSUPPORTED), (dict(dt=F32, ld=1026), UNSUPPORTED), (dict(dt=9), INVALID),
                             (dict(k=P + 8), UNSUPPORTED), (dict(v=P + 1), INVALID), (dict(kc=P + 4), UNSUPPORTED),
-                            (dict(slot=P + 2), INVALID), (dict(src=P + 1), INVALID), (dict(ks=P + 2), INVALID)])
+                            (dict(N=1 << 26), UNSUPPORTED), (dict(slot=P + 2), INVALID), (dict(src=P + 1), INVALID), (dict(ks=P + 2), INVALID)])
 def test_append_rejects(over, code):
     assert _call("treeflash_cache_append", APPEND, over) == code
 
@@ -99,7 +99,8 @@ ATTEND = dict(q=P, ldq=4096, k=P, v=P, ld=1024, mask=None, nl=None, ctx=P, table
                             (dict(q=P + 8), UNSUPPORTED), (dict(out=P + 2), UNSUPPORTED), (dict(out=P + 1), INVALID),
                             (dict(vc=P + 8), UNSUPPORTED), (dict(lse=P + 2), INVALID), (dict(nl=P + 1), INVALID),
                             (dict(ctx=P + 2), INVALID), (dict(ws=None), WORKSPACE), (dict(ws=P + 4), WORKSPACE),
-                            (dict(wsb=64), WORKSPACE), (dict(b=1 << 10, n=2000), INVALID)])
+                            (dict(wsb=64), WORKSPACE), (dict(b=1 << 10, n=2000), INVALID),
+                            (dict(b=200, n=4096, Hq=16, H=8, ldq=2048), UNSUPPORTED)])
 def test_attention_rejects(over, code):
     assert _call("treeflash_tree_attention", ATTEND, over) == code
 

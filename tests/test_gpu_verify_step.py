@@ -117,6 +117,27 @@ def test_sample_of_padded_and_offset_rows():
         check_sample(z, u, [0.8] * 4, [0, 20, 0, 300], [1.0, 0.9, 0.7, 1.0])
 
 
+def test_sample_of_many_rows():
+    """More rows than one dimension of a launch holds; settings that are not numbers are off, or the largest logit."""
+    rng = np.random.default_rng(31)
+    b, n, V = 211, 191, 7
+    nan = float("nan")
+    z = likely(rng, b, n, V, torch.float32, 2)
+    u = torch.tensor(rng.random((b, n)), dtype=torch.float32).cuda()
+    f = dict(dtype=torch.float32, device="cuda")
+    t = torch.full((b,), 1.0, **f)
+    p, m = torch.full((b,), nan, **f), torch.full((b,), nan, **f)
+    t[::3], t[1::3] = nan, float("inf")
+    tok, lp = binding.treeflash_sample(z, u, t, None, p, m)
+    top = z.argmax(-1).to(torch.int32)      # the first of equal ones
+    assert torch.equal(tok[::3], top[::3]) and not lp[::3].any()
+    # an infinite temperature makes all tokens alike: the u V-th of them
+    assert torch.equal(tok[1::3], (u[1::3].double() * V).floor().to(torch.int32))
+    w = torch.softmax(z[2::3].double(), -1).cumsum(-1)
+    want = (w <= u[2::3].double()[..., None]).sum(-1).clamp(max=V - 1)
+    assert torch.equal(tok[2::3].long(), want)
+
+
 def test_sample_shares_follow_the_probabilities():
     """Random numbers on a grid give each token its share of them, to one step of the grid."""
     z = torch.tensor([3.0, 1.0, -1.0, 2.0, 0.0], device="cuda").expand(1, 4096, 5).contiguous()
