@@ -14,10 +14,13 @@ namespace tf {
 // fp32.  Workgroup (position, up to kGroupRows heads of one key head, range): its
 // waves take 64 tokens in turn.  For the products q.k a lane is a token, for
 // the sums over values a dimension, so both read 16 contiguous codes a lane
-// and the weights change places through LDS.
+// and the weights change places through LDS.  New positions are few and their
+// rows wide: four lanes share one, sixteen go to a wave, and a wave's loads of
+// them are all in flight at once.
 template <int D>
 __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs a) {
     constexpr int kDims = D / kWave;
+    constexpr int kNew = kWave / 4;   // new positions a wave takes at once, four lanes each
     __shared__ float qs[kGroupRows][D];
     __shared__ float ps[kAttendWaves][kGroupRows][kWave];
     __shared__ float sm[kAttendWaves][kGroupRows], sl[kAttendWaves][kGroupRows];
@@ -106,29 +109,48 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
     }
     if ((int)blockIdx.z == sp.count - 1) {   // the new positions go with the last range
         const uint8_t* mask = a.mask != nullptr ? a.mask + (size_t)blockIdx.x * a.n : nullptr;
-        for (int j0 = wave * kWave; j0 < nl; j0 += kAttendThreads) {
-            const int j = j0 + lane;
+        for (int j0 = wave * kNew; j0 < nl; j0 += kNew * kAttendWaves) {
+            const int j = j0 + lane / 4, part = lane % 4;
             const bool sees = j < nl && (mask != nullptr ? mask[j] != 0 : j <= i);
-            unsigned long long todo = __ballot(sees);
+            unsigned long long todo = __ballot(sees && part == 0);
             if (todo == 0) continue;
-            float x[kGroupRows];
-            for (int g = 0; g < kGroupRows; ++g) x[g] = sees ? 0.f : neg_inf();
+            float x[kGroupRows] = {};
             if (sees) {
-                const float* k = static_cast<const float*>(a.k_new) + ((size_t)s * a.n + j) * a.ld_new + (size_t)hk * D;
-                for (int d = 0; d < D; ++d) {
-                    const float kv = k[d];
-                    for (int g = 0; g < kGroupRows; ++g) x[g] += qs[g][d] * kv;
-                }
+                const f32x4* k = reinterpret_cast<const f32x4*>(
+                    static_cast<const float*>(a.k_new) + ((size_t)s * a.n + j) * a.ld_new + (size_t)hk * D);
+                f32x4 kv[D / 16];
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) kv[c] = k[c * 4 + part];
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c)
+                    for (int g = 0; g < kGroupRows; ++g) {
+                        const float* qq = &qs[g][c * 16 + part * 4];
+                        x[g] += qq[0] * kv[c][0] + qq[1] * kv[c][1] + qq[2] * kv[c][2] + qq[3] * kv[c][3];
+                    }
+            }
+            for (int g = 0; g < kGroupRows; ++g) {
+                x[g] += __shfl_xor(x[g], 1);
+                x[g] += __shfl_xor(x[g], 2);
+                if (!sees || part != 0) x[g] = neg_inf();   // one lane of the four has the weight
             }
             weigh(x);
-            while (todo != 0) {
-                const int jj = __builtin_ctzll(todo);
-                todo &= todo - 1;
-                const float* v = static_cast<const float*>(a.v_new) + ((size_t)s * a.n + j0 + jj) * a.ld_new + (size_t)hk * D;
-                for (int c = 0; c < kDims; ++c) {
-                    const float val = v[c * kWave + lane];
-                    for (int g = 0; g < kGroupRows; ++g) o[g][c] += ps[wave][g][jj] * val;
+            while (todo != 0) {   // the rows attended to, four in flight
+                float val[4][kDims];
+                int at[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    at[r] = todo != 0 ? __builtin_ctzll(todo) : -1;
+                    todo &= todo - 1;
+                    const float* v = static_cast<const float*>(a.v_new) + ((size_t)s * a.n + j0 + max(at[r], 0) / 4) * a.ld_new + (size_t)hk * D;
+#pragma unroll
+                    for (int c = 0; c < kDims; ++c) val[r][c] = at[r] >= 0 ? v[c * kWave + lane] : 0.f;
                 }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (at[r] >= 0)
+#pragma unroll
+                        for (int c = 0; c < kDims; ++c)
+                            for (int g = 0; g < kGroupRows; ++g) o[g][c] += ps[wave][g][at[r]] * val[r][c];
             }
         }
     }

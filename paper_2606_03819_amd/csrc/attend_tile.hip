@@ -333,7 +333,33 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
         // the weights enter as a bf16 hi/lo pair (16 bits).  A value that is no
         // number must not reach the rows that do not attend to it, through
         // 0 * NaN: it is taken out of the product and added row by row.
-        for (int j0 = wave * 32; j0 < nl; j0 += kStep) {
+        const int jend = a.mask != nullptr ? nl : min(nl, (row0 + NQ * kTileRows - 1) / group + 1);   // a chain's last row ends it
+        // a bit for each of 8 positions from j that row n attends to
+        auto seen = [&](int n, int j) {
+            unsigned bits = 0;
+            if (a.mask != nullptr) {   // every byte's load in flight before the first is looked at
+                const uint8_t* mask = a.mask + ((size_t)s * a.n + pos[n]) * a.n;
+                uint8_t m[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m[e] = mask[min(j + e, nl - 1)];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) bits |= (m[e] != 0 ? 1u : 0u) << e;
+            } else {
+                bits = (1u << min(max(pos[n] - j + 1, 0), 8)) - 1u;
+            }
+            return bits & ((1u << min(max(nl - j, 0), 8)) - 1u);
+        };
+        for (int j0 = wave * 32; j0 < jend; j0 += kStep) {
+            const int jv = j0 + 8 * quarter;   // first of the lane's 8 positions
+            // Where a wave has several turns, one of which no row sees anything
+            // is left out (4 trees of 513 positions: 164 us, 190 with all turns);
+            // a single turn reads its keys without waiting for the mask.
+            if (a.mask != nullptr && nl > kStep) {
+                unsigned some = 0;
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) some |= seen(n, jv);
+                if (!__any(some != 0)) continue;
+            }
             f32x4 acc[NQ][2];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) acc[n][0] = acc[n][1] = f32x4{};
@@ -352,23 +378,11 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
                     }
                 }
             }
-            const int jv = j0 + 8 * quarter;   // first of the lane's 8 positions
             u32x4 ph[NQ], pl[NQ];
             float w[NQ][8];
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                unsigned sees = 0;
-                if (a.mask != nullptr) {   // every byte's load in flight before the first is looked at
-                    const uint8_t* mask = a.mask + ((size_t)s * a.n + pos[n]) * a.n;
-                    uint8_t m[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) m[j] = mask[min(jv + j, nl - 1)];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) sees |= (m[j] != 0 ? 1u : 0u) << j;
-                } else {
-                    sees = (1u << min(max(pos[n] - jv + 1, 0), 8)) - 1u;
-                }
-                sees &= (1u << min(max(nl - jv, 0), 8)) - 1u;
+                const unsigned sees = seen(n, jv);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) w[n][j] = sees >> j & 1 ? acc[n][j >> 2][j & 3] * qscale : neg_inf();
                 weigh<D>(w[n], 1.f, 0.f, 1.f, st[n], o[n]);
@@ -514,7 +528,6 @@ hipError_t launch_attend_tile(const AttendArgs& a, int D, hipStream_t stream) {
     const TileBlocks tb = tile_blocks(a.n, a.Hq, a.Hkv);
     const long long units = (long long)a.b * a.Hkv * a.splits;
     const long long grid = (units + 7) / 8 * 8 * tb.blocks;
-    if (grid > 0x7fffffffll) return hipErrorInvalidValue;
     const unsigned g = (unsigned)grid;
     if (D == 128) {
         if (tb.tiles == 1) launch_blocks<128, 1>(a, tb.blocks, g, stream);
