@@ -16,7 +16,7 @@
 //         largest, in steps of 1/16.
 // pick_kernel joins a row's slices.  `few` rows are ranked in one wave.  For
 // `whole` rows the steps' masses give each filter's border to one step; the
-// tokens of that step alone are looked up again and ranked, and once the
+// tokens of that step alone are looked up again and selected among, and once the
 // border is known the slices' masses give the slice that the draw falls into,
 // which is walked token by token.  Rows that this cannot serve (an infinite
 // logit, thousands of tokens in the border's step) are read once for each
