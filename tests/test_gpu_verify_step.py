@@ -106,6 +106,19 @@ def test_sample_numbers_outside_their_range_and_flat_rows():
         check_sample(z, u, **kw)
 
 
+@pytest.mark.parametrize("spread", [0.3, 0.8, 1.5])
+def test_sample_of_rows_of_little_spread(spread):
+    """Thousands of tokens within a sixteenth of the border's logit."""
+    rng = np.random.default_rng(17)
+    V = 151936
+    sets = [dict(p=0.9), dict(k=40000), dict(k=60000, p=0.5), dict(m=0.3), dict(p=0.9, m=0.25)]
+    get = lambda f, d: [s.get(f, d) for s in sets]  # noqa: E731
+    for dt in (torch.bfloat16, torch.float32):
+        z = torch.tensor(spread * rng.standard_normal((len(sets), 2, V)), dtype=torch.float32).to(dt).cuda()
+        u = torch.tensor(rng.random((len(sets), 2)), dtype=torch.float32).cuda()
+        check_sample(z, u, get("t", 1.0), get("k", 0), get("p", 1.0), get("m", 0.0))
+
+
 def test_sample_of_padded_and_offset_rows():
     rng = np.random.default_rng(5)
     for dt in (torch.bfloat16, torch.float32):
