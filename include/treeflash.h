@@ -394,6 +394,7 @@ tf_status_t treeflash_sample(const void *logits, long long ld, int b, int n, int
  *   start        out [b+1]: first of each sequence's tokens in the lists below
  *   page_start   out [b+1]: pages taken by the sequences before
  *   slot         out [max_tokens]: page * page_size + offset in the page
+ *                (max_tokens <= 2^30)
  *   position     out [max_tokens] or NULL: position in the sequence
  *   source       out [max_tokens] or NULL: row of the new keys and values,
  *                s*n + (0 for the root, 1 + node for accepted ones, j without

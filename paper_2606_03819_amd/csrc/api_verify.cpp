@@ -81,7 +81,8 @@ tf_status_t treeflash_cache_slots(const int32_t* context_len, const int32_t* add
     for (const void* p : need)
         if (p == nullptr || !aligned4(p)) return TF_ERR_INVALID_ARG;
     if (!opt4(accepted) || !opt4(position) || !opt4(source)) return TF_ERR_INVALID_ARG;
-    if (b < 1 || b > kMaxPositions || n < 0 || max_free < 1 || max_tokens < 1) return TF_ERR_INVALID_ARG;
+    if (b < 1 || b > kMaxPositions || n < 0 || max_free < 1 || max_tokens < 1 || max_tokens > 1 << 30)
+        return TF_ERR_INVALID_ARG;
     if (accepted != nullptr && (gamma < 1 || gamma > 255 || n < 1)) return TF_ERR_INVALID_ARG;
     if ((long long)b * n > 0x7fffffffll) return TF_ERR_INVALID_ARG;
     const tf_status_t st = page_status(page_size, max_pages);

@@ -179,11 +179,13 @@ __global__ __launch_bounds__(kFillThreads) void cache_fill_kernel(SlotsArgs a) {
     }
 }
 
-// One workgroup: the finished sequences' pages go onto the stack in order.
+// One workgroup: the finished sequences' pages go onto the stack in order, a
+// sequence a wave.
 __global__ __launch_bounds__(kPlanThreads) void cache_release_kernel(ReleaseArgs a) {
     __shared__ long long tmp[kPlanThreads / 64];
     __shared__ long long carry;
-    const int tid = threadIdx.x;
+    __shared__ int s_at[kPlanThreads], s_give[kPlanThreads];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int count = min(max(a.free_count[0], 0), a.max_free);
     if (tid == 0) carry = count;
     __syncthreads();
@@ -198,11 +200,14 @@ __global__ __launch_bounds__(kPlanThreads) void cache_release_kernel(ReleaseArgs
         }
         const long long t = block_scan(give, tmp);
         const long long at = carry + t - give;
-        for (int p = 0; p < give; ++p)
-            if (at + p < a.max_free) a.free_pages[at + p] = a.block_table[(size_t)s * a.max_pages + p];
+        s_at[tid] = (int)min(at, (long long)a.max_free);
+        s_give[tid] = (int)min((long long)give, (long long)a.max_free - s_at[tid]);
         if (s < a.b) a.new_len[s] = done ? 0 : len;
         __syncthreads();
         if (tid == kPlanThreads - 1) carry += t;
+        for (int q = wave; q < min(kPlanThreads, a.b - s0); q += kPlanThreads / kWave)
+            for (int p = lane; p < s_give[q]; p += kWave)
+                a.free_pages[s_at[q] + p] = a.block_table[(size_t)(s0 + q) * a.max_pages + p];
         __syncthreads();
     }
     if (tid == 0) a.new_free_count[0] = (int)min(carry, (long long)a.max_free);

@@ -55,7 +55,7 @@ SLOTS = dict(ctx=P, add=P, acc=P, free=P, fc=P, b=2, gamma=16, n=33, page=64, co
                          + [(dict(b=0), INVALID), (dict(gamma=0), INVALID), (dict(gamma=256), INVALID), (dict(n=0), INVALID),
                             (dict(n=-1), INVALID), (dict(page=0), INVALID), (dict(page=48), UNSUPPORTED),
                             (dict(page=256), UNSUPPORTED), (dict(page=8), UNSUPPORTED), (dict(cols=0), INVALID),
-                            (dict(cols=1 << 26), INVALID), (dict(max_free=0), INVALID), (dict(max_tokens=0), INVALID)])
+                            (dict(cols=1 << 26), INVALID), (dict(max_free=0), INVALID), (dict(max_tokens=0), INVALID), (dict(max_tokens=(1 << 30) + 1), INVALID)])
 def test_slots_rejects(over, code):
     assert _call("treeflash_cache_slots", SLOTS, over) == code
 

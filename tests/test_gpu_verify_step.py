@@ -264,6 +264,18 @@ def test_release_gives_pages_back_and_slots_take_them_again():
     assert out["slot"][:int(done.sum())].tolist() == [want[-1 - i] * page for i in range(int(done.sum()))]
 
 
+def test_release_of_long_sequences_stops_at_the_stack_s_end():
+    """More pages of a sequence than a wave has lanes; pages past the stack are dropped, what lies behind it stays."""
+    page, cols, b = 16, 300, 3
+    table = torch.arange(b * cols, dtype=torch.int32, device="cuda").view(b, cols)
+    ctx = i32([page * 200 - 3, page * 299 + 1, page * cols])
+    room = torch.full((1100,), -7, dtype=torch.int32, device="cuda")
+    free, fc = room[:600], i32([5])
+    binding.treeflash_cache_release(torch.ones((b,), dtype=torch.uint8, device="cuda"), ctx, table, free, fc, page)
+    want = [-7] * 5 + list(range(200)) + list(range(cols, 2 * cols)) + list(range(2 * cols, 3 * cols))
+    assert int(fc) == 600 and free.tolist() == want[:600] and (room[600:] == -7).all() and not ctx.any()
+
+
 # ------------------------------------------------------------------ append
 
 def check_append(cache, k, v, slot, source=None):
