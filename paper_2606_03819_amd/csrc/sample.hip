@@ -828,28 +828,43 @@ struct Whole {
 #pragma unroll
                     for (int e = 0; e < kPer; ++e)
                         if (first[d] + e < skip || first[d] + e >= end) hit &= ~(1u << (d * kPer + e));
-            if (__any(hit != 0)) {
-                int at = __popc(hit);
-                for (int o = 1; o < kWave; o <<= 1) {
-                    const int up = __shfl_up(at, o);
-                    if ((tid & 63) >= o) at += up;
-                }
-                int base = 0;
-                if ((tid & 63) == 63) base = atomicAdd(&sh.listed, at);
-                at += __builtin_amdgcn_readlane(base, 63) - __popc(hit);
+            // a wave's hits are counted a bit of the lanes' counts at a time
+            const int mine = __popc(hit);
+            int before = 0, all = 0;
 #pragma unroll
-                for (int d = 0; d < kDeep; ++d)
-#pragma unroll
-                    for (int e = 0; e < kPer; ++e)
-                        if (hit >> (d * kPer + e) & 1) {
-                            if (at < kBorderList)
-                                sh.list[at] = (u64)logit_key(vector_at<T>(raw[d], e)) << 32 | (uint32_t)~(first[d] + e - skip);
-                            ++at;
-                        }
+            for (int b = 0; b < 6; ++b) {
+                const unsigned long long m = __ballot(mine >> b & 1);
+                before += lanes_below(m) << b;
+                all += __popcll(m) << b;
+            }
+            if (all == 0) continue;
+            int base = 0;
+            if ((tid & 63) == 0) base = atomicAdd(&sh.listed, all);
+            int at = __builtin_amdgcn_readfirstlane(base) + before;
+            for (; hit != 0; hit &= hit - 1, ++at) {
+                const int bit = __builtin_ctz(hit), i = i0 + bit / kPer * kSampleThreads;
+                if (at < kBorderList) sh.list[at] = sh.holds[i / (kSlice / kPer)] * kSlice + i % (kSlice / kPer) * kPer + bit % kPer - skip;
             }
         }
         __syncthreads();
-        return sh.listed <= kBorderList;
+        const int n = sh.listed;
+        if (n > kBorderList) return false;
+        // ids so far: now their logits, several loads in flight
+        constexpr int kKeys = 4;
+        for (int i0 = tid; i0 < n; i0 += kKeys * kSampleThreads) {
+            int id[kKeys];
+            uint32_t key[kKeys];
+#pragma unroll
+            for (int d = 0; d < kKeys; ++d) {
+                id[d] = (int)sh.list[min(i0 + d * kSampleThreads, n - 1)];
+                key[d] = i0 + d * kSampleThreads < n ? key_at(row, id[d]) : 0u;
+            }
+#pragma unroll
+            for (int d = 0; d < kKeys; ++d)
+                if (i0 + d * kSampleThreads < n) sh.list[i0 + d * kSampleThreads] = (u64)key[d] << 32 | (uint32_t)~id[d];
+        }
+        __syncthreads();
+        return true;
     }
     __device__ u64 weight_of(u64 entry) const { return weight(place(key_f32((uint32_t)(entry >> 32))).rest); }
 
