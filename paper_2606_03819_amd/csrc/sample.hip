@@ -820,7 +820,7 @@ struct Whole {
 #pragma unroll
                 for (int e = 0; e < kPer; ++e) {
                     const float z = vector_at<T>(raw[d], e);
-                    hit |= z >= lo && z <= hi ? 1u << (d * kPer + e) : 0u;
+                    hit |= __builtin_amdgcn_fmed3f(z, lo, hi) == z ? 1u << (d * kPer + e) : 0u;
                 }
 #pragma unroll
             for (int d = 0; d < kDeep; ++d)   // at the row's ends, what is no logit of it
