@@ -22,8 +22,8 @@
 // logit, thousands of tokens in the border's step) are read once for each
 // byte of their keys instead (hard_row).
 //
-// Measured: 528 rows of 151936 bf16 with settings of all kinds 73 us of scan
-// (2.2 TB/s; bound by 64-bit arithmetic and LDS atomics) and 90 of pick (each
+// Measured: 528 rows of 151936 bf16 with settings of all kinds 75 us of scan
+// (2.1 TB/s; bound by 64-bit arithmetic and LDS atomics) and 79 of pick (each
 // row's chain of filters, and the second read); one row with top-k 20: 5.5
 // and 9.7.
 #include "common.hpp"
@@ -47,7 +47,7 @@ constexpr int kSurvivors = 2048;
 // Tokens of a border's step that LDS holds beside a second workgroup of its CU
 // (which registers allow): all of a step wherever the logits over T spread by
 // 0.6 or more in 150 thousand.  A list of 2048 sent rows of spread 1 to
-// hard_row: one row 714 us, 86 now; 528 rows 1824, 252 now.
+// hard_row: one row 714 us, 72 now; 528 rows 1824, 226 now.
 constexpr int kBorderList = 6144;
 constexpr uint32_t kKeyNone = 0x007fffffu;        // -inf's key: that and below is no token
 typedef unsigned long long u64;
