@@ -405,6 +405,14 @@ def test_attention_of_a_large_tree():
 
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_attention_of_many_positions_in_padded_batches(dt):
+    """Several turns over the new positions, of which a row sees few, in batches that use a part of them."""
+    rng = np.random.default_rng(18)
+    attention_case(rng, dt, 3, 301, 2, 1, 128, 32, [0, 70, 33], lens=[301, 129, 257])
+    attention_case(rng, dt, 2, 290, 6, 2, 64, 16, [9, 0], chain=True, lens=[290, 128])
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
 def test_attention_scales_of_very_different_size(dt):
     attention_case(np.random.default_rng(15), dt, 2, 5, 4, 2, 64, 16, [400, 33], spread=12)
 
