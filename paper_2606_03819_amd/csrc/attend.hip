@@ -11,44 +11,46 @@
 
 namespace tf {
 
-// fp32.  Workgroup (position, up to kGroupRows heads of one key head, range): its
+// fp32.  Workgroup (position, up to G heads of one key head, range): its
 // waves take 64 tokens in turn.  For the products q.k a lane is a token, for
 // the sums over values a dimension, so both read 16 contiguous codes a lane
 // and the weights change places through LDS.  New positions are few and their
 // rows wide: four lanes share one, sixteen go to a wave, and a wave's loads of
-// them are all in flight at once.
-template <int D>
+// them are all in flight at once.  What bounds it: the latency of these loads
+// while there are few positions (2 trees of 100 over 500 tokens, 4 heads a key
+// head: 29 us, 57 with the queries in registers), then fp32 arithmetic.
+template <int D, int G>
 __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs a) {
     constexpr int kDims = D / kWave;
     constexpr int kNew = kWave / 4;   // new positions a wave takes at once, four lanes each
-    __shared__ float qs[kGroupRows][D];
-    __shared__ float ps[kAttendWaves][kGroupRows][kWave];
-    __shared__ float sm[kAttendWaves][kGroupRows], sl[kAttendWaves][kGroupRows];
-    __shared__ float so[kAttendWaves][kGroupRows][D];
+    __shared__ float qs[G][D];
+    __shared__ float ps[kAttendWaves][G][kWave];
+    __shared__ float sm[kAttendWaves][G], sl[kAttendWaves][G];
+    __shared__ float so[kAttendWaves][G][D];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int s = blockIdx.x / a.n, i = blockIdx.x % a.n;
     const int nl = new_of(a, s);
     const int ctx = context_of(a, s);
     const Split sp = split_context(ctx, a.splits);
     if (i >= nl || (int)blockIdx.z >= sp.count) return;   // uniform
-    const int group = a.Hq / a.Hkv, blocks = (group + kGroupRows - 1) / kGroupRows;
-    const int hk = blockIdx.y / blocks, g0 = (blockIdx.y % blocks) * kGroupRows;
-    const int ng = min(kGroupRows, group - g0);
+    const int group = a.Hq / a.Hkv, blocks = (group + G - 1) / G;
+    const int hk = blockIdx.y / blocks, g0 = (blockIdx.y % blocks) * G;
+    const int ng = min(G, group - g0);
     const int head0 = hk * group + g0;
     const float* q = static_cast<const float*>(a.q) + (size_t)blockIdx.x * a.ld_q + (size_t)head0 * D;
-    for (int e = tid; e < kGroupRows * D; e += kAttendThreads)
+    for (int e = tid; e < G * D; e += kAttendThreads)
         qs[e / D][e % D] = e / D < ng ? q[e] * (a.scale * kLog2e) : 0.f;
     __syncthreads();
 
-    float m[kGroupRows], l[kGroupRows], o[kGroupRows][kDims];
-    for (int g = 0; g < kGroupRows; ++g) {
+    float m[G], l[G], o[G][kDims];
+    for (int g = 0; g < G; ++g) {
         m[g] = neg_inf();
         l[g] = 0.f;
         for (int c = 0; c < kDims; ++c) o[g][c] = 0.f;
     }
     // the lane's products x become weights: LDS gets them, m, l and o follow
     auto weigh = [&](const float* x) {
-        for (int g = 0; g < kGroupRows; ++g) {
+        for (int g = 0; g < G; ++g) {
             const float mn = fmaxf(m[g], wave_max(x[g]));
             const float back = mn == neg_inf() ? 1.f : exp2f(m[g] - mn);   // 0 from an empty start
             const float p = exp2f(x[g] - (mn == neg_inf() ? 0.f : mn));   // a NaN stays one
@@ -62,10 +64,14 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
     const int32_t* table = a.block_table + (size_t)s * a.max_pages;
     const int lo = blockIdx.z * sp.chunk, hi = min(ctx, lo + sp.chunk);
     for (int t0 = lo + wave * kWave; t0 < hi; t0 += kAttendThreads) {
+        // The queries are read from LDS for every 64 tokens.  Without this the
+        // compiler keeps all G * D of them in registers (330 for four heads of
+        // 64), and one wave a SIMD waits out every load.
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const int t = t0 + lane;
         int id = t < hi ? table[t / a.page] : -1;
         if (id >= a.num_pages) id = -1;
-        float x[kGroupRows] = {};
+        float x[G] = {};
         if (id >= 0) {
             const size_t head = (size_t)id * a.Hkv + hk;
             const u32x4* k = reinterpret_cast<const u32x4*>(a.k_cache + head * a.page * D + (size_t)(t & (a.page - 1)) * D);
@@ -73,16 +79,16 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
                 const u32x4 w = k[c];
                 for (int e = 0; e < 4; ++e) {
                     const f32pair u = e4m3_pair<false>(w[e]), v = e4m3_pair<true>(w[e]);
-                    for (int g = 0; g < kGroupRows; ++g) {
+                    for (int g = 0; g < G; ++g) {
                         const float* qq = &qs[g][c * 16 + e * 4];
                         x[g] += qq[0] * u[0] + qq[1] * u[1] + qq[2] * v[0] + qq[3] * v[1];
                     }
                 }
             }
             const float ks = a.k_scale[head];
-            for (int g = 0; g < kGroupRows; ++g) x[g] *= ks;
+            for (int g = 0; g < G; ++g) x[g] *= ks;
         } else {
-            for (int g = 0; g < kGroupRows; ++g) x[g] = neg_inf();
+            for (int g = 0; g < G; ++g) x[g] = neg_inf();
         }
         weigh(x);
         for (int part = 0; part < kWave / 16; ++part) {   // 16 tokens lie in one page
@@ -101,7 +107,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
                     for (int j = 0; j < 4; ++j) {
                         const int tt = e * 4 + j;
                         const float val = first + tt < hi ? y[j] * vs : 0.f;   // what lies behind may be NaN
-                        for (int g = 0; g < kGroupRows; ++g) o[g][c] += ps[wave][g][part * 16 + tt] * val;
+                        for (int g = 0; g < G; ++g) o[g][c] += ps[wave][g][part * 16 + tt] * val;
                     }
                 }
             }
@@ -114,7 +120,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
             const bool sees = j < nl && (mask != nullptr ? mask[j] != 0 : j <= i);
             unsigned long long todo = __ballot(sees && part == 0);
             if (todo == 0) continue;
-            float x[kGroupRows] = {};
+            float x[G] = {};
             if (sees) {
                 const f32x4* k = reinterpret_cast<const f32x4*>(
                     static_cast<const float*>(a.k_new) + ((size_t)s * a.n + j) * a.ld_new + (size_t)hk * D);
@@ -123,12 +129,12 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
                 for (int c = 0; c < D / 16; ++c) kv[c] = k[c * 4 + part];
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c)
-                    for (int g = 0; g < kGroupRows; ++g) {
+                    for (int g = 0; g < G; ++g) {
                         const float* qq = &qs[g][c * 16 + part * 4];
                         x[g] += qq[0] * kv[c][0] + qq[1] * kv[c][1] + qq[2] * kv[c][2] + qq[3] * kv[c][3];
                     }
             }
-            for (int g = 0; g < kGroupRows; ++g) {
+            for (int g = 0; g < G; ++g) {
                 x[g] += __shfl_xor(x[g], 1);
                 x[g] += __shfl_xor(x[g], 2);
                 if (!sees || part != 0) x[g] = neg_inf();   // one lane of the four has the weight
@@ -150,11 +156,11 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
                     if (at[r] >= 0)
 #pragma unroll
                         for (int c = 0; c < kDims; ++c)
-                            for (int g = 0; g < kGroupRows; ++g) o[g][c] += ps[wave][g][at[r]] * val[r][c];
+                            for (int g = 0; g < G; ++g) o[g][c] += ps[wave][g][at[r]] * val[r][c];
             }
         }
     }
-    for (int g = 0; g < kGroupRows; ++g) {
+    for (int g = 0; g < G; ++g) {
         const float sum = wave_sum(l[g]);
         if (lane == 0) sm[wave][g] = m[g], sl[wave][g] = sum;
         for (int c = 0; c < kDims; ++c) so[wave][g][c * kWave + lane] = o[g][c];
@@ -249,6 +255,19 @@ int splits_of(int b, int n, int Hq, int Hkv, int page, int max_pages, bool bf16)
     return most_splits((long long)b * n * Hkv * row_blocks(Hq, Hkv), 1024, max_pages, page);
 }
 
+// A key head's G is the smallest that holds its group, since every product,
+// maximum and exponent is made for all G heads (11 sequences of 25 positions, 2
+// heads a key head: 24 us, 37 by four; 4 of 33 over 2000 tokens, single heads of
+// 64: 40 us, 70 by four).
+template <int D>
+void launch_rows(const AttendArgs& a, hipStream_t stream) {
+    const int group = a.Hq / a.Hkv;
+    const dim3 grid(a.b * a.n, a.Hkv * row_blocks(a.Hq, a.Hkv), a.splits), w(kAttendThreads);
+    if (group == 1) hipLaunchKernelGGL((attend_rows_kernel<D, 1>), grid, w, 0, stream, a);
+    else if (group == 2) hipLaunchKernelGGL((attend_rows_kernel<D, 2>), grid, w, 0, stream, a);
+    else hipLaunchKernelGGL((attend_rows_kernel<D, kGroupRows>), grid, w, 0, stream, a);
+}
+
 template <class T>
 hipError_t launch_merge(const AttendArgs& a, int D, hipStream_t stream) {
     const dim3 grid((unsigned)(((long long)a.b * a.n * a.Hq + kAttendWaves - 1) / kAttendWaves));
@@ -270,9 +289,8 @@ hipError_t launch_tree_attention(AttendArgs a, int D, bool bf16, hipStream_t str
     if (bf16) {
         e = launch_attend_tile(a, D, stream);
     } else {
-        const dim3 grid(a.b * a.n, a.Hkv * row_blocks(a.Hq, a.Hkv), a.splits);
-        if (D == 128) hipLaunchKernelGGL(attend_rows_kernel<128>, grid, dim3(kAttendThreads), 0, stream, a);
-        else hipLaunchKernelGGL(attend_rows_kernel<64>, grid, dim3(kAttendThreads), 0, stream, a);
+        if (D == 128) launch_rows<128>(a, stream);
+        else launch_rows<64>(a, stream);
         e = hipGetLastError();
     }
     if (e != hipSuccess || a.splits == 1) return e;

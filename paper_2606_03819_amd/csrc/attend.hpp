@@ -9,7 +9,7 @@ namespace tf {
 
 constexpr int kAttendThreads = 256;
 constexpr int kAttendWaves = kAttendThreads / kWave;
-constexpr int kGroupRows = 4;   // query heads of one position that a workgroup of the row kernel serves
+constexpr int kGroupRows = 4;   // most query heads of one position that a workgroup of the row kernel serves
 
 // The ranges that a context of `ctx` tokens is split into: at most `most`, of
 // kSplitLeast tokens at least, each a multiple of 64 but the last.
