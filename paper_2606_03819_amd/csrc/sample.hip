@@ -917,10 +917,12 @@ struct Whole {
     // The listed entry, at least `from`, at which those from the largest down
     // reach `target` weights (BY_MASS) or entries, found nine bits at a time
     // among the bits in which what is left differs; the last one if all
-    // together do not.
+    // together do not.  The first always counts: a target of nothing (top_p
+    // 0), which a bin without entries would reach, is one unit of weight.
     template <bool BY_MASS>
     __device__ u64 reach(double target, u64 from) {
         const int tid = threadIdx.x;
+        target = fmax(target, 1.);
         u64 lo = from, hi = ~0ull, above = 0;
         for (;;) {
             u64 mn = ~0ull, mx = 0;

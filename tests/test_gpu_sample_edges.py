@@ -1,0 +1,47 @@
+"""Sampling at the ends of what its settings and steps allow, against the 64-bit oracle."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_03819_amd import binding
+from test_gpu_verify_step import check_sample, likely
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.bfloat16, torch.float32]
+
+
+def written(b, n):
+    """Outputs that no sample leaves as they are."""
+    return dict(token=torch.full((b, n), -7, dtype=torch.int32, device="cuda"),
+                logprob=torch.full((b, n), 7.0, device="cuda"))
+
+
+def crowned(kind, V):
+    """Rows whose largest logits are tied, lie within a sixteenth of one another, or are all there is."""
+    rng = np.random.default_rng(V)
+    z = rng.standard_normal(V).clip(-3, 3)
+    if kind == "tied":
+        z[[5, 9]] = 8.0
+    elif kind == "tied far apart":
+        z[[V - 2, 7, V // 2]] = 8.0
+    elif kind == "near":
+        z[[11, 3, 200, 17]] = 8.0, 7.96875, 8.0, 7.9375
+    else:
+        z[:] = 0.5
+    return z
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("k", [0, 100, 3])
+def test_no_mass_keeps_the_first_token(k, dt):
+    for V in (900, 3000, 40000):
+        kinds = ["tied", "tied far apart", "near", "flat"]
+        z = np.stack([np.stack([crowned(kind, V)] * 2) for kind in kinds])
+        zt = torch.tensor(z).to(dt).cuda()
+        u = torch.tensor([[0.0, 0.97]] * len(kinds), dtype=torch.float32).cuda()
+        for p in (0.0, -0.0, -1.0, -float("inf"), 1e-30, 1e-7):
+            print(f"V {V} k {k} p {p} {dt}", flush=True)
+            tok, lp = check_sample(zt, u, k=[k] * len(kinds), p=[p] * len(kinds), **written(len(kinds), 2))
+            assert tok.tolist() == [[5, 5], [7, 7], [11, 11], [0, 0]] and lp.abs().max() < 2.0 ** -30
+            check_sample(zt, u, t=[0.8, 1.0, 3.0, 0.1], k=[k] * len(kinds), p=[p] * len(kinds), m=[0.5] * len(kinds))
