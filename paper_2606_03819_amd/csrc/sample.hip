@@ -1052,7 +1052,9 @@ struct Whole {
         }
         if (set.mp > 0.f) {
             const double floor = (double)set.mp;
-            const double d = (double)top - rint(ytop + kPerUnit * log(floor));
+            // ytop is rounded where `top` is not: at an end of the largest
+            // logit's step, and min_p 1, this would be the step above it
+            const double d = fmax((double)top - rint(ytop + kPerUnit * log(floor)), 0.);
             const int j = d < (double)kSteps ? (int)d : kSteps;
             if (j <= edge && j < kSteps) {
                 if (j != listed && !list_step(j)) return false;

@@ -45,3 +45,25 @@ def test_no_mass_keeps_the_first_token(k, dt):
             tok, lp = check_sample(zt, u, k=[k] * len(kinds), p=[p] * len(kinds), **written(len(kinds), 2))
             assert tok.tolist() == [[5, 5], [7, 7], [11, 11], [0, 0]] and lp.abs().max() < 2.0 ** -30
             check_sample(zt, u, t=[0.8, 1.0, 3.0, 0.1], k=[k] * len(kinds), p=[p] * len(kinds), m=[0.5] * len(kinds))
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+def test_min_p_of_one_keeps_the_largest_alone(dt):
+    """Largest logits at the ends of their steps of a sixteenth of T: whichever step rounding gives them, they are kept."""
+    V = 5000
+    temps = [1.5, 3.0, 6.0, 0.75, 0.3, 0.7, 0.1, 5.0]
+    rows = np.zeros((len(temps), 24, V))
+    for s, t in enumerate(temps):
+        for i in range(24):
+            rng = np.random.default_rng(100 * s + i)
+            top = float(torch.tensor((i - 8 + 0.5) * float(np.float32(t)) / 16).to(dt))
+            step = abs(top) * float(torch.finfo(dt).eps)
+            rows[s, i] = top - step - rng.random(V) * t
+            rows[s, i, rng.integers(0, V, 3)] = top
+            rows[s, i, 40] = top - step   # and the nearest below it
+    z = torch.tensor(rows).to(dt).cuda()
+    u = torch.tensor(np.random.default_rng(1).random((len(temps), 24)), dtype=torch.float32).cuda()
+    for kw in (dict(), dict(p=[0.9] * 8), dict(k=[300] * 8), dict(k=[300] * 8, p=[0.01] * 8)):
+        print(dt, kw, flush=True)
+        check_sample(z, u, temps, m=[1.0] * 8, **kw, **written(8, 24))
+        check_sample(z, u, temps, m=[1.0 - 2.0 ** -24] * 8, **kw, **written(8, 24))
