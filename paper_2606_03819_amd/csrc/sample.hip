@@ -455,9 +455,11 @@ __device__ void scan_few(const Chunk<T>& c, int first, int skip, int n, ChunkLis
 // Where a logit lies: y = 16 z / T, its step b (the nearest integer) and exp
 // of what is left, |rest| <= 1/32, by its series to the 6th power (error 2^-47).
 // Adding 1.5 * 2^52 rounds to an integer and leaves it in the sum's low bits,
-// which takes three operations for step and rest.  Rows whose largest |y| is
-// 2^20 or more (kFar) are left to hard_row: there a step is no longer far
-// above the logits' own rounding.
+// which takes three operations for step and rest.  Rows whose largest y is
+// not within kFar are left to hard_row: there a step is no longer far above the
+// logits' own rounding.  The scan leaves out slices by the same test of their
+// own largest, so a row's has to be farther inside at the lower end than
+// any slice that matters to it can be below it.
 constexpr double kRound = 0x1.8p52;
 constexpr double kFar = 0x1p20;
 struct Step {
@@ -1186,7 +1188,7 @@ __global__ __launch_bounds__(kSampleThreads, 4) void pick_kernel(SampleArgs a, i
             return;
         }
         const double per = kPerUnit / (double)set.t, ytop = (double)largest * per;
-        if (fabs(ytop) < kFar) {
+        if (ytop < kFar && ytop > 2 * kSteps - kFar) {
             const T* row = static_cast<const T*>(a.logits) + (size_t)r * a.ld;
             const double one = ldexp(1., bits);
             Whole<T> w{a, set, data, sh.whole, tmp, row, slices, Chunk<T>::skip_of(row), r, per, ytop, one,

@@ -67,3 +67,17 @@ def test_min_p_of_one_keeps_the_largest_alone(dt):
         print(dt, kw, flush=True)
         check_sample(z, u, temps, m=[1.0] * 8, **kw, **written(8, 24))
         check_sample(z, u, temps, m=[1.0 - 2.0 ** -24] * 8, **kw, **written(8, 24))
+
+
+def test_rows_whose_slices_straddle_the_largest_distance():
+    """16 z / T just above -2^20 in one slice and just below it in the others, a few units of T apart."""
+    rng = np.random.default_rng(5)
+    V, t = 40000, float(np.float32(1e-3))
+    limit = -t * 2.0 ** 16
+    z = np.full((6, 4, V), limit) - 2e-3 - rng.random((6, 4, V)) * 4e-3
+    for i, above in enumerate((1e-5, 1e-4, 1e-3, 2.9e-2)):
+        z[:, i, rng.integers(0, V, 3)] = limit + above
+    z[5] = -z[5]                        # the other end: none of these rows is within it
+    zt = torch.tensor(z, dtype=torch.float32).cuda()
+    u = torch.tensor(rng.random((6, 4)), dtype=torch.float32).cuda()
+    check_sample(zt, u, [t] * 6, [0, 0, 0, 500, 20000, 0], [1.0, 0.9, 1.0, 1.0, 0.7, 1.0], [0.0, 0.0, 0.01, 0.0, 0.0, 0.0])
