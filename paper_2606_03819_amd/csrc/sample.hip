@@ -14,13 +14,16 @@
 //         the ones that can be among the row's best k;
 //   whole (else) -- masses of the slice by the value's distance from its
 //         largest, in steps of 1/16.
-// pick_kernel joins a row's slices.  `few` rows are ranked in one wave.  For
-// `whole` rows the steps' masses give each filter's border to one step; the
-// tokens of that step alone are looked up again and selected among, and once the
-// border is known the slices' masses give the slice that the draw falls into,
-// which is walked token by token.  Rows that this cannot serve (an infinite
-// logit, thousands of tokens in the border's step) are read once for each
-// byte of their keys instead (hard_row).
+// pick_kernel joins a row's slices.  `few` rows are ranked by waves, 64 entries
+// at a time.  For `whole` rows the steps' masses give each filter's border to
+// one step; the tokens of that step alone are looked up again and selected
+// among, and once the border is known the slices' masses give the slice that
+// the draw falls into, which is walked token by token.  Rows that this cannot
+// serve are read once for each byte of their keys instead (hard_row): `whole`
+// rows whose largest 16 |z| / T is 2^20 or more (an infinite logit; T below 3e-4
+// at a logit of 20), or with more than 6144 tokens in a border's step; `few`
+// rows whose lists leave more than 8064 entries (thousands of ties in 64 lists
+// or more).
 //
 // Measured: 528 rows of 151936 bf16 with settings of all kinds 75 us of scan
 // (2.1 TB/s; bound by 64-bit arithmetic and LDS atomics) and 79 of pick (each
@@ -43,7 +46,11 @@ constexpr int kFew = 64;                          // tokens that one wave ranks
 constexpr int kList = 128;                        // of a chunk, entries kept
 constexpr int kSteps = 512;                       // of 1/16: e^-32 of the largest is no weight (2^-46)
 constexpr int kPerUnit = 16;
-constexpr int kSurvivors = 2048;
+// Entries of a row's lists that are ranked in LDS: all of them where the row has
+// no more than 63 lists, which cannot be bounded for top-k 64 by their largest
+// alone (with 2048, top-k 50 of 50257 logits went to hard_row: four rows 211
+// us, 23 now).
+constexpr int kSurvivors = (kFew - 1) * kList;
 // Tokens of a border's step that LDS holds beside a second workgroup of its CU
 // (which registers allow): all of a step wherever the logits over T spread by
 // 0.6 or more in 150 thousand.  A list of 2048 sent rows of spread 1 to
@@ -632,6 +639,7 @@ __device__ __forceinline__ void each_entry(const SliceData* data, int lists, F f
 
 struct FewShared {
     u64 list[kSurvivors];
+    u64 rank[kSampleWaves][kWave];
     int count;
 };
 
@@ -675,8 +683,9 @@ __device__ void draw_few(const SampleArgs& a, const RowSettings& set, u64 best, 
 }
 
 // Joins a row's lists.  The n-th largest of the lanes' largest list heads
-// bounds what can be among the best n; those survivors are ranked by one wave,
-// 64 at a time.  Returns false where too many survive.
+// bounds what can be among the best n (fewer lists than n: everything can);
+// the waves rank these survivors 64 at a time, each its share, and one joins
+// them.  Returns false where too many survive.
 __device__ bool pick_few(const SampleArgs& a, const RowSettings& set, const SliceData* data, int slices, int n,
                          int bits, FewShared& sh, u64* tmp) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -701,9 +710,16 @@ __device__ bool pick_few(const SampleArgs& a, const RowSettings& set, const Slic
     __syncthreads();
     const int count = sh.count;
     if (count > kSurvivors) return false;
+    auto ranked = [&](int i) { return wave_sort(i + lane < count ? sh.list[i + lane] : 0ull); };
+    u64 best = 0;
+    if (wave * kWave < count) {
+        best = ranked(wave * kWave);
+        for (int i = wave * kWave + kSampleThreads; i < count; i += kSampleThreads) best = wave_merge(best, ranked(i));
+        sh.rank[wave][lane] = best;
+    }
+    __syncthreads();
     if (wave == 0) {
-        u64 best = wave_sort(lane < count ? sh.list[lane] : 0ull);
-        for (int i = kWave; i < count; i += kWave) best = wave_merge(best, wave_sort(i + lane < count ? sh.list[i + lane] : 0ull));
+        for (int w = 1; w < min(kSampleWaves, (count + kWave - 1) / kWave); ++w) best = wave_merge(best, sh.rank[w][lane]);
         draw_few(a, set, best, n, bits);
     }
     return true;

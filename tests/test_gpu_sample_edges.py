@@ -81,3 +81,48 @@ def test_rows_whose_slices_straddle_the_largest_distance():
     zt = torch.tensor(z, dtype=torch.float32).cuda()
     u = torch.tensor(rng.random((6, 4)), dtype=torch.float32).cuda()
     check_sample(zt, u, [t] * 6, [0, 0, 0, 500, 20000, 0], [1.0, 0.9, 1.0, 1.0, 0.7, 1.0], [0.0, 0.0, 0.01, 0.0, 0.0, 0.0])
+
+
+@pytest.mark.parametrize("V,k", [(50257, 50), (64000, 50), (92544, 50), (100352, 64), (128256, 64), (30000, 64), (125000, 62)])
+def test_top_k_of_more_tokens_than_the_row_has_lists(V, k):
+    """As many lists of 2048 logits as k or fewer: their largest alone give no bound, so thousands of entries are joined."""
+    rng = np.random.default_rng(V)
+    sets = [dict(k=k), dict(k=k, p=0.95, t=0.6), dict(k=k, m=0.02), dict(k=k - 1, t=2.0)]
+    get = lambda f, d: [s.get(f, d) for s in sets]  # noqa: E731
+    for dt in DTYPES:
+        for steps in (None, 4):
+            z = likely(rng, len(sets), 2, V, dt, steps)
+            u = torch.tensor(rng.random((len(sets), 2)), dtype=torch.float32).cuda()
+            check_sample(z, u, get("t", 1.0), get("k", 0), get("p", 1.0), get("m", 0.0))
+
+
+def test_top_k_takes_as_long_over_a_smaller_vocabulary():
+    """Rows of 50 thousand logits take no longer than rows of 152 thousand do, whose lists are more than k (a third
+    is allowed for: reading byte by byte takes many times as long)."""
+    def microseconds(V):
+        z = likely(np.random.default_rng(1), 4, 1, V, torch.bfloat16)
+        u, k = torch.full((4, 1), 0.5, device="cuda"), torch.full((4,), 50, dtype=torch.int32, device="cuda")
+        ws = binding.alloc_workspace(binding.treeflash_sample_workspace_bytes(4, 1, V), z.device)
+        out = written(4, 1)
+        call = lambda: binding.treeflash_sample(z, u, top_k=k, workspace=ws, **out)  # noqa: E731
+        call()
+        graph = torch.cuda.CUDAGraph()
+        side = torch.cuda.Stream()
+        with torch.cuda.graph(graph, stream=side):
+            for _ in range(20):
+                call()
+        best = 1e9
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            graph.replay()
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b) * 50)
+        return best
+
+    long = microseconds(151936)
+    for V in (50257, 64000, 100352):
+        short = microseconds(V)
+        print(f"top-k 50 of {V}: {short:.1f} us, of 151936: {long:.1f}", flush=True)
+        assert short < long * 4 / 3
