@@ -272,9 +272,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
         if (kOneSet && more) load_keys<D, PAGE>(next.k, a, to, lane_k);
         __builtin_amdgcn_sched_barrier(0);   // the values' operands are made after the weights: else they spill
         const int e = (int)(__float_as_uint(v_scale) >> 23) - 127;
-        const float ks = k_scale * qscale, inv = __uint_as_float((uint32_t)(127 - e) << 23);
         const bool part = !place.whole();   // uniform
         const int left = place.left(quarter);
+        // where a quarter has no token, the scale is a page's that may never have been written
+        const float ks = k_scale * qscale, inv = left == 0 ? 1.f : __uint_as_float((uint32_t)(127 - e) << 23);
         u32x4 p[NQ];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {

@@ -1,0 +1,46 @@
+"""Attention over caches whose other pages hold nothing of use, and over contexts near the largest length."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_03819_amd import binding
+from verify_step import check_attention, i32, make_cache, tables, tree_masks
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.bfloat16, torch.float32]
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scales_of_pages_that_no_sequence_holds(D, page, dt):
+    """Neither codes nor scales of other pages count: not behind a sequence's last token, and not where a table entry
+    is no page, page 0 among them."""
+    rng = np.random.default_rng(D + page)
+    b, n, Hq, H = 5, 3, 4, 2
+    ctx = [page + 5, 3 * page - 7, 1, page, 0]
+    cols = 5
+    order = 1 + rng.permutation(30)                       # page 0 and most others are nobody's
+    table = np.zeros((b, cols), dtype=np.int32)
+    at = 0
+    for s, c in enumerate(ctx):
+        held = -(-c // page)
+        table[s, :held] = order[at:at + held]
+        table[s, held:] = rng.choice([-1, 0, 31, 32, 10 ** 9, order[-1]], cols - held)
+        at += held
+    table[1, 1] = -5                                      # a hole in the middle
+    owned = sorted({int(table[s, p]) for s, c in enumerate(ctx) for p in range(-(-c // page)) if 0 <= table[s, p] < 32})
+    clean = make_cache(rng, 32, H, page, D)
+    q, k, v = (torch.tensor(rng.standard_normal((b, n, h, D))).to(dt).cuda() for h in (Hq, H, H))
+    mask = torch.tensor(tree_masks(rng, b, n)).cuda()
+    others = torch.ones((32,), dtype=torch.bool, device="cuda")
+    others[owned] = False
+    for bad in (float("nan"), float("inf"), -float("inf"), 0.0, -1.0, 3e38):
+        print(D, page, dt, bad, flush=True)
+        cache = {f: t.clone() for f, t in clean.items()}
+        for f in ("k", "v"):
+            cache[f + "_scale"][others] = bad
+            cache[f + "_cache"].view(torch.uint8)[others] = 127
+        out, lse = binding.treeflash_tree_attention(q, k, v, mask, i32(ctx), i32(table), **cache, scale=0.2)
+        check_attention(out, lse, q, k, v, mask, ctx, i32(table), clean, 0.2)
