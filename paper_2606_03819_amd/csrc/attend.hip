@@ -209,8 +209,9 @@ __global__ __launch_bounds__(kAttendThreads) void merge_kernel(AttendArgs a) {
         lp = ml[1];
     }
     const float m = wave_max(mp);
-    const float f = mp == neg_inf() ? (lp == 0.f ? 0.f : lp) : exp2f(mp - m);   // a sum that is no number stays one
-    const float l = wave_sum(lp * f);
+    // a sum that is no number stays one; in halves, since 2^(mp - m) alone may be nothing where lp is 2^64
+    const float h = mp == neg_inf() ? (lp == 0.f ? 0.f : lp) : exp2f(0.5f * (mp - m)), f = h * h;
+    const float l = wave_sum(lp * h * h);
     float o[D / kWave] = {};
     constexpr int kDeep = 8;
     for (int s0 = 0; s0 < count; s0 += kDeep) {
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(kAttendThreads) void merge_kernel(AttendArgs a) {
         }
     }
     for (int c = 0; c < D / kWave; ++c) store_out(a.out, row * D + c * kWave + lane, l == 0.f ? 0.f : o[c] / l, sizeof(T) == 2);
-    if (lane == 0 && a.lse != nullptr) a.lse[row] = lse_of(m, l);
+    if (lane == 0 && a.lse != nullptr) a.lse[row] = lse_of(sizeof(T) == 2 ? m + kLift : m, l);
 }
 
 namespace {

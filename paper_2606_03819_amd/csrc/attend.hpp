@@ -34,9 +34,14 @@ __device__ __forceinline__ int new_of(const AttendArgs& a, int s) {
     return a.new_len == nullptr ? a.n : min(max(a.new_len[s], 0), a.n);
 }
 
+// The matrix kernel's weights are made 2^kLift as large (at most 2^62, for the
+// slack its maximum has; at least 2^-126, which is 2^-182 under the largest), and
+// its running maxima are held less kLift.
+constexpr int kLift = 56;
+
 // Partials of split contexts: for row r = (s*n + i)*Hq + head and range sp
-// the D sums, and behind all of them the running maximum (base 2) and the sum
-// of weights.
+// the D sums, and behind all of them the running maximum (base 2; of the matrix
+// kernel less kLift) and the sum of weights.
 __device__ __forceinline__ float* part_sums(const AttendArgs& a, size_t row, int sp, int D) {
     return a.part + ((size_t)sp * a.b * a.n * a.Hq + row) * D;
 }

@@ -18,7 +18,10 @@
 // the scales, the products take the bare codes, and the denominator adds
 // 2^(u - m) * 2^-e in fp32.  m is only raised when it is passed by more than
 // kSlack, since raising it means scaling all of O^T and a maximum over the
-// lanes that share a row.
+// lanes that share a row.  Beside pages of scale 2^64 the weights of pages of
+// 2^-64 (those of zeros) are 2^-128 and less: nothing to the products, but not to
+// the denominator.  So weights are made 2^kLift as large, and the products' are
+// brought back as they are rounded to fp16.
 //
 // What bounds it: with few rows the reads (64 sequences' single tokens over up
 // to 8192: 152 us, 5.2 TB/s of cache); with many the chain through a tile at
@@ -129,33 +132,36 @@ __device__ __forceinline__ float scale_of(const float* scale, const TilePlace<PA
     else return scale[at.head[0]];
 }
 
-// The running softmax of a lane's query row (the four lanes of a row hold the same m).
+// The running softmax of a lane's query row (the four lanes of a row hold the
+// same m, which stands here less kLift).
 struct Running {
     float m, l;
 };
 
-// x[8] become weights 2^(x ks + e - m); O^T and l follow a raised m.  ks is
-// not negative, so the largest x has the largest weight; -inf is not there
-// (ks is 1 then).  `inv`: what the denominator's weights carry, 2^-e.
-template <int D>
+// x[8] become weights 2^(x ks + e - m + LIFT); O^T and l follow a raised m.  ks
+// is not negative, so the largest x has the largest weight; -inf is not there
+// (ks is 1 then).  `inv`: what the denominator's weights carry, 2^-(e + LIFT).
+template <int D, int LIFT>
 __device__ __forceinline__ void weigh(float (&x)[8], float ks, float e, float inv, Running& s, f32x4 (&o)[D / 16]) {
     float top = x[0];
 #pragma unroll
     for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
     top = fmaf(top, ks, e);
-    if (__any(top > s.m + kSlack)) {   // also from an empty start (-inf)
+    if (__any(top > s.m + (kSlack + kLift))) {   // also from an empty start (-inf)
         top = fmaxf(top, lane_xor<16>(top));
         top = fmaxf(top, lane_xor<32>(top));
-        const bool raise = top > s.m + kSlack;
-        const float f = raise ? __builtin_amdgcn_exp2f(s.m - top) : 1.f;
+        const bool raise = top > s.m + (kSlack + kLift);
+        top -= kLift;
+        // in halves: l is 2^64 after quiet pages alone, and that under a loud one's m
+        const float h = raise ? __builtin_amdgcn_exp2f(0.5f * (s.m - top)) : 1.f, f = h * h;
         s.m = raise ? top : s.m;
-        s.l *= f;
+        s.l = s.l * h * h;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c)
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[c][j] *= f;
     }
-    const float off = s.m == neg_inf() ? 0.f : e - s.m;
+    const float off = (s.m == neg_inf() ? 0.f : e - s.m) - (kLift - LIFT);
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -275,7 +281,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
         const bool part = !place.whole();   // uniform
         const int left = place.left(quarter);
         // where a quarter has no token, the scale is a page's that may never have been written
-        const float ks = k_scale * qscale, inv = left == 0 ? 1.f : __uint_as_float((uint32_t)(127 - e) << 23);
+        const float ks = k_scale * qscale, inv = left == 0 ? 1.f : __uint_as_float((uint32_t)(127 - kLift - e) << 23);
+        constexpr float kDrop = 1.f / (1ull << kLift);
         u32x4 p[NQ];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -289,9 +296,9 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
                 k1 = 1.f;
                 e1 = 0.f;
             }
-            weigh<D>(u, k1, e1, inv, st[n], o[n]);
+            weigh<D, kLift>(u, k1, e1, inv, st[n], o[n]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) p[n][j] = f16_pair(u[2 * j], u[2 * j + 1]);
+            for (int j = 0; j < 4; ++j) p[n][j] = f16_pair(u[2 * j] * kDrop, u[2 * j + 1] * kDrop);
         }
         if (part) {   // what lies behind the tokens may be NaN
             const int l0 = min(left, 4), l1 = max(left - 4, 0);
@@ -386,7 +393,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
                 const unsigned sees = seen(n, jv);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) w[n][j] = sees >> j & 1 ? acc[n][j >> 2][j & 3] * qscale : neg_inf();
-                weigh<D>(w[n], 1.f, 0.f, 1.f, st[n], o[n]);
+                weigh<D, 0>(w[n], 1.f, 0.f, 1.f, st[n], o[n]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t h = f32x2_to_bf16x2_bits(w[n][2 * j], w[n][2 * j + 1]);
@@ -481,7 +488,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
             f32x4 x = {0.f, 0.f, 0.f, 0.f};
             for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, sm[w][r]);
             for (int w = 0; w < kAttendWaves; ++w) {
-                lt += sm[w][r] == neg_inf() ? sl[w][r] : sl[w][r] * __builtin_amdgcn_exp2f(sm[w][r] - m);
+                const float h = sm[w][r] == neg_inf() ? 1.f : __builtin_amdgcn_exp2f(0.5f * (sm[w][r] - m));
+                lt += sl[w][r] * h * h;
                 const f32x4 v = *reinterpret_cast<const f32x4*>(&shared[w].sums[r][d]);
                 for (int k = 0; k < 4; ++k) x[k] += v[k];
             }
@@ -493,7 +501,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
                 v.x = f32x2_to_bf16x2_bits(none ? 0.f : x[0] * g, none ? 0.f : x[1] * g);
                 v.y = f32x2_to_bf16x2_bits(none ? 0.f : x[2] * g, none ? 0.f : x[3] * g);
                 *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to * D + d) = v;
-                if (d == 0 && a.lse != nullptr) a.lse[to] = lse_of(m, lt);
+                if (d == 0 && a.lse != nullptr) a.lse[to] = lse_of(m + kLift, lt);
             } else {
                 *reinterpret_cast<f32x4*>(part_sums(a, to, range, D) + d) = x;
                 if (d == 0) {

@@ -44,3 +44,26 @@ def test_scales_of_pages_that_no_sequence_holds(D, page, dt):
             cache[f + "_cache"].view(torch.uint8)[others] = 127
         out, lse = binding.treeflash_tree_attention(q, k, v, mask, i32(ctx), i32(table), **cache, scale=0.2)
         check_attention(out, lse, q, k, v, mask, ctx, i32(table), clean, 0.2)
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("page", [16, 64])
+def test_value_scales_at_both_ends_of_their_range(page, dt):
+    """Pages whose values are nothing (the smallest scale) beside pages of the largest: the former's tokens have their
+    part in the sum of weights all the same."""
+    rng = np.random.default_rng(page)
+    n, Hq, H, D, pages = 2, 4, 2, 64, 8
+    for loud in (64, 40, 62):
+        for first in (0, 1):
+            cache = make_cache(rng, pages, H, page, D, 0)
+            cache["v_scale"][:] = 2.0 ** loud
+            quiet = torch.arange(pages, device="cuda") % 2 == first
+            cache["v_scale"][quiet] = 2.0 ** -64
+            cache["v_cache"].view(torch.uint8)[quiet] = 0
+            table = i32([list(range(pages)), [3, 0, 2, 1, 5, 4, 6, 7]])
+            ctx = [pages * page - 3, 2 * page]
+            q, k = (torch.tensor(rng.standard_normal((2, n, h, D))).to(dt).cuda() for h in (Hq, H))
+            v = torch.zeros_like(k)
+            print(page, dt, loud, first, flush=True)
+            out, lse = binding.treeflash_tree_attention(q, k, v, None, i32(ctx), table, **cache, scale=0.01)
+            check_attention(out, lse, q, k, v, None, ctx, table, cache, 0.01)
