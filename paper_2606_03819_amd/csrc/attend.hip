@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_rows_kernel(AttendArgs 
     };
 
     const int32_t* table = a.block_table + (size_t)s * a.max_pages;
-    const int lo = blockIdx.z * sp.chunk, hi = min(ctx, lo + sp.chunk);
+    const int lo = sp.begin(blockIdx.z), hi = sp.end(blockIdx.z, ctx);
     for (int t0 = lo + wave * kWave; t0 < hi; t0 += kAttendThreads) {
         // The queries are read from LDS for every 64 tokens.  Without this the
         // compiler keeps all G * D of them in registers (330 for four heads of

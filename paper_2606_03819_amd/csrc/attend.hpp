@@ -1,6 +1,7 @@
 // Attention over the paged 8-bit cache: what its kernels share.
 #pragma once
 
+#include "attend_split.hpp"
 #include "common.hpp"
 #include "e4m3.hpp"
 #include "launch.hpp"
@@ -10,22 +11,6 @@ namespace tf {
 constexpr int kAttendThreads = 256;
 constexpr int kAttendWaves = kAttendThreads / kWave;
 constexpr int kGroupRows = 4;   // most query heads of one position that a workgroup of the row kernel serves
-
-// The ranges that a context of `ctx` tokens is split into: at most `most`, of
-// kSplitLeast tokens at least, each a multiple of 64 but the last.
-constexpr int kSplitLeast = 256, kMostSplits = 64;
-struct Split {
-    int chunk, count;
-};
-__host__ __device__ inline Split split_context(int ctx, int most) {
-    int e = (ctx + kSplitLeast - 1) / kSplitLeast;
-    e = e < most ? e : most;
-    e = e > 1 ? e : 1;
-    int chunk = ((ctx + e - 1) / e + 63) & ~63;
-    chunk = chunk > 64 ? chunk : 64;
-    const int count = (ctx + chunk - 1) / chunk;
-    return {chunk, count > 1 ? count : 1};
-}
 
 __device__ __forceinline__ int context_of(const AttendArgs& a, int s) {
     return min(max(a.context_len[s], 0), a.max_pages * a.page);

@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_tile_kernel(AttendAr
     }
     const float qscale = fabsf(a.scale) * kLog2e;
     const int32_t* table = a.block_table + (size_t)s * a.max_pages;
-    const int lo = range * sp.chunk, hi = min(ctx, lo + sp.chunk);
+    const int lo = sp.begin(range), hi = sp.end(range, ctx);
     constexpr int kStep = kAttendWaves * 32;
     const int kt = 8 * (col >> 2) + (col & 3);   // token of the lane's key row (s = 0)
     const int lane_k = (kt & (PAGE - 1)) * D + 16 * quarter;

@@ -67,3 +67,23 @@ def test_value_scales_at_both_ends_of_their_range(page, dt):
             print(page, dt, loud, first, flush=True)
             out, lse = binding.treeflash_tree_attention(q, k, v, None, i32(ctx), table, **cache, scale=0.01)
             check_attention(out, lse, q, k, v, None, ctx, table, cache, 0.01)
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("page", [16, 128])
+def test_contexts_near_the_largest_length(page, dt):
+    """Tables of 2^31 tokens whose entries are pages at their two ends only: the last range ends with the context."""
+    rng = np.random.default_rng(page)
+    n, Hq, H, D = 2, 2, 1, 64
+    cols = 0x7fffff00 // page
+    table = torch.full((1, cols), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = 2
+    cache = make_cache(rng, 4, H, page, D)
+    q, k, v = (torch.tensor(rng.standard_normal((1, n, h, D))).to(dt).cuda() for h in (Hq, H, H))
+    for ctx in (cols * page, cols * page - 7, cols * page - (1 << 25) - 5, (1 << 31) - (1 << 26) + 3):
+        last = (ctx - 1) // page
+        table[0, last], few = 1, page + (ctx - 1) % page + 1
+        print(page, dt, ctx, flush=True)
+        out, lse = binding.treeflash_tree_attention(q, k, v, None, i32([ctx]), table, **cache, scale=0.2)
+        check_attention(out, lse, q, k, v, None, [few], i32([[2, 1]]), cache, 0.2)
+        table[0, last] = -1
