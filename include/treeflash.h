@@ -382,7 +382,8 @@ tf_status_t treeflash_sample(const void *logits, long long ld, int b, int n, int
  *   context_len  [b] int32 tokens held before
  *   add_len      [b] int32 tokens gained; with `accepted`, the accept_len of
  *                treeflash_accept, and the sequence gains 1 + add_len tokens:
- *                the root and its accepted nodes
+ *                the root and its accepted nodes, or nothing where it is -1 (a
+ *                sequence that sits the step out)
  *   accepted     [b, gamma] int32 of treeflash_accept, or NULL (gamma unused)
  *   n            positions a sequence has in the arrays of new keys and values
  *                (B + 1 with `accepted`), or 0 where their rows are packed

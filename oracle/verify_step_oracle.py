@@ -92,7 +92,7 @@ def cache_slots(context_len, add_len, accepted, free_pages, free_count: int, blo
                 page_start=np.zeros(b + 1, int), block_table=block_table.copy(), slot=np.full(max_tokens, -1),
                 position=np.full(max_tokens, -1), source=np.full(max_tokens, -1))
     gamma = accepted.shape[1] if accepted is not None else 0
-    if (free_count < 0 or free_count > len(free_pages) or min(context_len) < 0 or min(add_len) < 0
+    if (free_count < 0 or free_count > len(free_pages) or min(context_len) < 0 or min(add) < 0
             or (accepted is not None and max(add_len) > gamma) or (n > 0 and max(add) > n)):
         return dict(none, status=1)
     if sum(add) > max_tokens:

@@ -535,7 +535,7 @@ def treeflash_cache_slots(context_len: torch.Tensor, add_len: torch.Tensor, free
                           accepted: Optional[torch.Tensor] = None, n: int = 0, out: Optional[dict] = None):
     """Pages, slots and positions of the tokens that each sequence gains, from lengths on the GPU: add_len [b]
     tokens, or with `accepted` [b, gamma] (treeflash_accept's, add_len its accept_len) the root and the accepted
-    nodes of a tree input of n positions.  block_table is updated in place.  `out` may hold context_len and
+    nodes of a tree input of n positions, nothing where add_len is -1.  block_table is updated in place.  `out` may hold context_len and
     free_count themselves to update them in place; status 0 says that the pages sufficed."""
     func = "treeflash_cache_slots"
     dev = _gpu("block_table", block_table)
@@ -827,8 +827,9 @@ class PagedCache:
         cache.advance(walk)
         for each layer: cache.append(layer, k, v)
 
-    A prompt is added with cache.extend(add_len, max_tokens) and then append for
-    each layer.  `status` reads 0 where the last advance or extend found the
+    A slot without a sequence (released, or not yet filled) sits the step out:
+    0 in advance's `active`, and 0 in attend's new_len.  A prompt is added with
+    cache.extend(add_len, max_tokens) and then append for each layer.  `status` reads 0 where the last advance or extend found the
     pages it needed; otherwise nothing was taken and append writes nothing."""
 
     def __init__(self, layers: int, b: int, n: int, gamma: int, Hq: int, Hkv: int, D: int, num_pages: int, max_pages: int,
@@ -851,6 +852,8 @@ class PagedCache:
         self.context_len = torch.zeros((b,), **i32)
         self.free_count = torch.full((1,), num_pages, **i32)
         self._step_lists = self._lists(b * (gamma + 1))
+        self._active = torch.ones((b,), dtype=torch.bool, device=dev)
+        self._gain, self._none = torch.empty((b,), **i32), torch.full((), -1, **i32)
         self.slots = self._step_lists   # of the last advance or extend
         self.out = torch.empty((b, n, Hq, D), dtype=dtype, device=dev)
         self.lse = torch.empty((b, n, Hq), dtype=torch.float32, device=dev)
@@ -873,10 +876,19 @@ class PagedCache:
                                         self.v[layer], self.k_scale[layer], self.v_scale[layer], scale, new_len,
                                         self.workspace, self.out if out is None else out, self.lse if lse is None else lse)
 
-    def advance(self, walk: Dict[str, torch.Tensor]) -> dict:
-        """Pages and slots of the root and the accepted nodes of treeflash_accept's result."""
+    def advance(self, walk: Dict[str, torch.Tensor], active: Optional[torch.Tensor] = None) -> dict:
+        """Pages and slots of the root and the accepted nodes of treeflash_accept's result; sequences with
+        active [b] (uint8 or bool) 0 gain nothing."""
+        gain = walk["accept_len"]
+        if active is not None:
+            func = "PagedCache.advance"
+            _gpu("active", active)
+            _arg(func, "active", active, torch.bool if active.dtype is torch.bool else torch.uint8, (self.b,), self.dev)
+            _arg(func, "accept_len", gain, torch.int32, (self.b,), self.dev)
+            torch.ne(active, 0, out=self._active)
+            gain = torch.where(self._active, gain, self._none, out=self._gain)
         self.slots = self._step_lists
-        return treeflash_cache_slots(self.context_len, walk["accept_len"], self.free_pages, self.free_count,
+        return treeflash_cache_slots(self.context_len, gain, self.free_pages, self.free_count,
                                      self.block_table, self.page_size, self.b * (self.gamma + 1),
                                      accepted=walk["accepted"], n=self.n, out=self.slots)
 

@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(SlotsArgs a, i
         ctx = a.context_len[s];
         add = a.add_len[s];
         need = 0;
-        if (ctx < 0 || add < 0 || (extra && add > a.gamma) || (a.n > 0 && (long long)add + extra > a.n)) {
+        if (ctx < 0 || add < -extra || (extra && add > a.gamma) || (a.n > 0 && (long long)add + extra > a.n)) {
             wrong = 1;
             continue;
         }
