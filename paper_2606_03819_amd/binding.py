@@ -851,6 +851,7 @@ class PagedCache:
         self.free_pages = torch.arange(num_pages - 1, -1, -1, **i32)   # page 0 is taken first
         self.context_len = torch.zeros((b,), **i32)
         self.free_count = torch.full((1,), num_pages, **i32)
+        self.status = torch.zeros((1,), **i32)   # of the last advance or extend that the GPU did, captured ones too
         self._step_lists = self._lists(b * (gamma + 1))
         self._active = torch.ones((b,), dtype=torch.bool, device=dev)
         self._gain, self._none = torch.empty((b,), **i32), torch.full((), -1, **i32)
@@ -863,11 +864,7 @@ class PagedCache:
         return {"context_len": self.context_len, "free_count": self.free_count,
                 "start": torch.empty((self.b + 1,), **e), "page_start": torch.empty((self.b + 1,), **e),
                 "slot": torch.empty((max_tokens,), **e), "position": torch.empty((max_tokens,), **e),
-                "source": torch.empty((max_tokens,), **e), "status": torch.empty((1,), **e)}
-
-    @property
-    def status(self) -> torch.Tensor:
-        return self.slots["status"]
+                "source": torch.empty((max_tokens,), **e), "status": self.status}
 
     def attend(self, layer: int, q, k_new, v_new, mask, scale: float, new_len=None, out=None, lse=None):
         """Attention of the tree's positions in one layer, into `out` and `lse` (held buffers if not given,

@@ -95,3 +95,26 @@ def test_released_sequences_sit_out_of_paged_steps():
     for bad, err in ((active.int(), TypeError), (active[:3], ValueError), (active.cpu(), ValueError), ([1, 0, 1, 0], TypeError)):
         with pytest.raises(err):
             pc.advance(walk, active=bad)
+
+
+def test_status_is_the_last_call_s_on_the_gpu():
+    """A captured advance replayed after an extend, and an extend after a replay, each leave their own status."""
+    b, gamma, page = 2, 3, 16
+    pc = binding.PagedCache(1, b, 5, gamma, 2, 1, 64, num_pages=6, max_pages=5, page_size=page)
+    walk = dict(accept_len=i32([3, 2]), accepted=i32([[0, 1, 2], [0, 3, -1]]))
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        pc.advance(walk)
+    pc.extend(i32([14, 10]), 24)
+    assert int(pc.status) == 0 and int(pc.free_count) == 4
+    graph.replay()
+    assert int(pc.status) == 0 and pc.context_len.tolist() == [18, 13] and int(pc.free_count) == 3
+    pc.extend(i32([100, 0]), 100)                       # outgrows its table
+    assert int(pc.status) == 3
+    graph.replay()
+    assert int(pc.status) == 0 and pc.context_len.tolist() == [22, 16] and int(pc.free_count) == 3
+    pc.extend(i32([42, 0]), 42)                         # to the end of a page, of the last but one page
+    assert int(pc.status) == 0 and pc.context_len.tolist() == [64, 16] and int(pc.free_count) == 1
+    for _ in range(3):
+        graph.replay()                                  # two more pages: there is one
+        assert int(pc.status) == 4 and pc.context_len.tolist() == [64, 16]
