@@ -868,10 +868,14 @@ class PagedCache:
 
     def attend(self, layer: int, q, k_new, v_new, mask, scale: float, new_len=None, out=None, lse=None):
         """Attention of the tree's positions in one layer, into `out` and `lse` (held buffers if not given,
-        which the next call overwrites)."""
+        which the next call overwrites).  Of another number of positions than n, a prompt's part or single tokens,
+        the workspace and what is not given are allocated."""
+        workspace = None
+        if q.shape[1] == self.n:
+            workspace, out, lse = self.workspace, self.out if out is None else out, self.lse if lse is None else lse
         return treeflash_tree_attention(q, k_new, v_new, mask, self.context_len, self.block_table, self.k[layer],
                                         self.v[layer], self.k_scale[layer], self.v_scale[layer], scale, new_len,
-                                        self.workspace, self.out if out is None else out, self.lse if lse is None else lse)
+                                        workspace, out, lse)
 
     def advance(self, walk: Dict[str, torch.Tensor], active: Optional[torch.Tensor] = None) -> dict:
         """Pages and slots of the root and the accepted nodes of treeflash_accept's result; sequences with

@@ -118,3 +118,33 @@ def test_status_is_the_last_call_s_on_the_gpu():
     for _ in range(3):
         graph.replay()                                  # two more pages: there is one
         assert int(pc.status) == 4 and pc.context_len.tolist() == [64, 16]
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_attention_of_other_numbers_of_positions_than_the_cache_s(dt):
+    """Prompt chunks and single tokens through a cache made for trees: a smaller n can need a larger workspace."""
+    rng = np.random.default_rng(41)
+    b, n, Hq, H, D, page = 2, 33, 8, 2, 64, 16
+    pc = binding.PagedCache(1, b, n, 4, Hq, H, D, num_pages=400, max_pages=250, page_size=page, dtype=dt)
+    cache = dict(k_cache=pc.k[0], v_cache=pc.v[0], k_scale=pc.k_scale[0], v_scale=pc.v_scale[0])
+    ctx = [0, 0]
+    for chunk, lens in ((70, None), (1, None), (33, [33, 20]), (1, [0, 1]), (200, [200, 3]), (7, None), (33, None)):
+        qkv = torch.tensor(rng.standard_normal((b, chunk, Hq + 2 * H, D))).to(dt).cuda()
+        q, k, v = qkv[:, :, :Hq], qkv[:, :, Hq:Hq + H], qkv[:, :, Hq + H:]
+        kw, left = {}, None
+        if lens is not None:
+            left = (torch.full((b, chunk, Hq, D), 7.0, dtype=dt).cuda(), torch.full((b, chunk, Hq), 7.0).cuda())
+            kw = dict(new_len=i32(lens), out=left[0].clone(), lse=left[1].clone())
+        out, lse = pc.attend(0, q, k, v, None, 0.1, **kw)
+        assert out.shape == q.shape and lse.shape == q.shape[:3]
+        assert (out.data_ptr() == pc.out.data_ptr()) == (chunk == n and lens is None)
+        check_attention(out, lse, q, k, v, None, ctx, pc.block_table, cache, 0.1, lens, left)
+        add = lens or [chunk] * b
+        pc.extend(i32(add), b * chunk, n=chunk)
+        pc.append(0, k, v)
+        ctx = [c + a for c, a in zip(ctx, add)]
+        assert int(pc.status) == 0 and pc.context_len.tolist() == ctx
+    with pytest.raises(ValueError):
+        pc.attend(0, q[:1], k[:1], v[:1], None, 0.1)
+    with pytest.raises(ValueError):
+        pc.attend(0, q[:, :, :4].contiguous(), k, v, None, 0.1)
