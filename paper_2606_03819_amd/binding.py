@@ -866,13 +866,14 @@ class PagedCache:
                 "slot": torch.empty((max_tokens,), **e), "position": torch.empty((max_tokens,), **e),
                 "source": torch.empty((max_tokens,), **e), "status": self.status}
 
-    def attend(self, layer: int, q, k_new, v_new, mask, scale: float, new_len=None, out=None, lse=None):
+    def attend(self, layer: int, q, k_new, v_new, mask, scale: float, new_len=None, out=None, lse=None, workspace=None):
         """Attention of the tree's positions in one layer, into `out` and `lse` (held buffers if not given,
-        which the next call overwrites).  Of another number of positions than n, a prompt's part or single tokens,
-        the workspace and what is not given are allocated."""
-        workspace = None
+        which the next call overwrites).  The held workspace, too, is one for all layers: calls that may run at the
+        same time, on two streams or in two replayed graphs, each need an `out`, `lse` and `workspace` of their own.
+        Of another number of positions than n, a prompt's part or single tokens, what is not given is allocated."""
         if q.shape[1] == self.n:
-            workspace, out, lse = self.workspace, self.out if out is None else out, self.lse if lse is None else lse
+            workspace = self.workspace if workspace is None else workspace
+            out, lse = self.out if out is None else out, self.lse if lse is None else lse
         return treeflash_tree_attention(q, k_new, v_new, mask, self.context_len, self.block_table, self.k[layer],
                                         self.v[layer], self.k_scale[layer], self.v_scale[layer], scale, new_len,
                                         workspace, out, lse)

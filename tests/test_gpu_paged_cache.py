@@ -148,3 +148,31 @@ def test_attention_of_other_numbers_of_positions_than_the_cache_s(dt):
         pc.attend(0, q[:1], k[:1], v[:1], None, 0.1)
     with pytest.raises(ValueError):
         pc.attend(0, q[:, :, :4].contiguous(), k, v, None, 0.1)
+
+
+def test_layers_attended_to_on_two_streams_at_once():
+    """Contexts in many ranges, each stream with a workspace and outputs of its own."""
+    rng = np.random.default_rng(42)
+    b, n, Hq, H, D, page, ctx = 2, 5, 4, 1, 128, 64, [9000, 4001]
+    pc = binding.PagedCache(2, b, n, 4, Hq, H, D, num_pages=220, max_pages=150, page_size=page)
+    pc.extend(i32(ctx), sum(ctx))
+    for i in range(2):
+        kv = torch.tensor(rng.standard_normal((sum(ctx), 2 * H, D))).to(torch.bfloat16).cuda()
+        pc.append(i, kv[:, :H], kv[:, H:])
+    qkv = torch.tensor(rng.standard_normal((b, n, Hq + 2 * H, D))).to(torch.bfloat16).cuda()
+    q, k, v = qkv[:, :, :Hq], qkv[:, :, Hq:Hq + H], qkv[:, :, Hq + H:]
+    want = [[t.clone() for t in pc.attend(i, q, k, v, None, 0.1)] for i in range(2)]
+    own = [dict(out=torch.empty_like(pc.out), lse=torch.empty_like(pc.lse), workspace=torch.empty_like(pc.workspace))
+           for _ in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for kw in own:
+            kw["out"].zero_(), kw["lse"].zero_(), kw["workspace"].fill_(255)
+        torch.cuda.synchronize()
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                pc.attend(i, q, k, v, None, 0.1, **own[i])
+        torch.cuda.synchronize()
+        for kw, w in zip(own, want):
+            assert torch.equal(kw["out"], w[0]) and torch.equal(kw["lse"], w[1])
