@@ -366,9 +366,11 @@ size_t treeflash_sample_workspace_bytes(int b, int n, int V);
  * kept are the first top_k of them, of these the shortest prefix that holds
  * top_p of their mass, and of these the ones with w_v >= min_p (the first
  * token always stays).  The token is the first one, by id, at which the
- * running sum of the kept w exceeds uniform times their total.  Weights and
- * sums are exact to about 2^-44 of the largest weight, whatever the order of
- * the additions, so a result does not depend on the launch.
+ * running sum of the kept w exceeds uniform times their total.  A weight is
+ * exact to 2^-m of the largest, m = min(46, 63 - bits of V) (45 at V = 151936,
+ * 40 at 2^22), and those of less than 2^-m may count as nothing; a sum over V
+ * tokens is exact to V times that.  Additions are of integers or in a fixed
+ * order, so a result does not depend on the launch.
  * NaN counts as -inf, and -inf is never drawn: a row of them alone gives token
  * -1 and logprob -inf.  Where +inf occurs its tokens share the whole mass.
  * V <= 2^22. */

@@ -5,8 +5,10 @@
 // order, so the kept set is "keys above a border, and the first few ids of
 // those on it".  Sums are exact far beyond fp32, as integers or in 64 bits: a
 // draw turns on the borders between up to V running sums, and with V errors
-// of 2^-24 one row in a hundred would draw another token.  Whatever is added
-// by atomics is an integer, so that the order of additions changes nothing.
+// of 2^-24 one row in a hundred would draw another token.  A weight's own error
+// is at most 2^-46 of the largest, or half a unit of the integers, 2^(bits of V
+// - 63), if that is more.  Whatever is added by atomics is an integer, so that
+// the order of additions changes nothing.
 //
 // Two launches.  scan_kernel reads the logits once, a slice of 8192 at a
 // time, and leaves what the row's settings need:
@@ -25,10 +27,13 @@
 // rows whose lists leave more than 8064 entries (thousands of ties in 64 lists
 // or more).
 //
-// Measured: 528 rows of 151936 bf16 with settings of all kinds 75 us of scan
-// (2.1 TB/s; bound by 64-bit arithmetic and LDS atomics) and 79 of pick (each
-// row's chain of filters, and the second read); one row with top-k 20: 5.5
-// and 9.7.
+// Measured: 528 rows of 151936 bf16 with settings of all kinds 76 us of scan
+// (2.1 TB/s; bound by 64-bit arithmetic, vector instructions issue in 65% of its
+// cycles, and LDS atomics) and 80 of pick (each row's chain of filters, and the
+// second read: its waves wait 62% of the time); one row with top-k 20: 5.5 and
+// 9.7.  A pick is one workgroup a row, so that few rows with a filter but no
+// small top-k take nearly what many do: one row with top-p 56 us a call, 64 rows
+// 69.
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -44,7 +49,7 @@ constexpr int kScanWaves = kScanThreads / kWave;
 constexpr int kChunk = kSlice / kScanWaves;       // of a wave
 constexpr int kFew = 64;                          // tokens that one wave ranks
 constexpr int kList = 128;                        // of a chunk, entries kept
-constexpr int kSteps = 512;                       // of 1/16: e^-32 of the largest is no weight (2^-46)
+constexpr int kSteps = 512;                       // of 1/16: e^-32 of the largest (2^-46) counts as no weight
 constexpr int kPerUnit = 16;
 // Entries of a row's lists that are ranked in LDS: all of them where the row has
 // no more than 63 lists, which cannot be bounded for top-k 64 by their largest
