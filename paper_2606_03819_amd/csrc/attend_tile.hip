@@ -24,10 +24,13 @@
 // brought back as they are rounded to fp16.
 //
 // What bounds it: with few rows the reads (64 sequences' single tokens over up
-// to 8192: 152 us, 5.2 TB/s of cache); with many the chain through a tile at
-// two waves a SIMD -- 64 codes a lane turned into operands, shared by the NQ row
-// tiles, then 8 exponents a row tile (16 sequences, 33 positions of 4 heads a
-// key head, up to 16384 tokens: 200 us, 0.55 PFLOP/s; without any loads 187).
+// to 8192: 153 us, 5.2 TB/s of cache); with many the latency of a tile's chain --
+// products, the codes' conversion, which the NQ row tiles share, 8 exponents a row
+// tile, products -- at the one or two waves a SIMD that registers allow: 16
+// sequences, 33 positions of 4 heads a key head, up to 16384 tokens take 205 us
+// (0.53 PFLOP/s), vector instructions issue in 46% of the cycles, the matrix units
+// are busy in 24%, a wave waits a third of its time for data and a third for its
+// turn, and 18% of the CUs' time is the uneven contexts' end.
 #include "attend.hpp"
 
 namespace tf {
