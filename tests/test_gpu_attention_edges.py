@@ -87,3 +87,20 @@ def test_contexts_near_the_largest_length(page, dt):
         out, lse = binding.treeflash_tree_attention(q, k, v, None, i32([ctx]), table, **cache, scale=0.2)
         check_attention(out, lse, q, k, v, None, [few], i32([[2, 1]]), cache, 0.2)
         table[0, last] = -1
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+def test_calls_repeat_themselves_whatever_the_workspace_holds(dt):
+    rng = np.random.default_rng(11)
+    for b, n, ctx in ((1, 1, [4000]), (3, 33, [1500, 0, 701]), (2, 150, [64, 900])):
+        table, pages, _ = tables(rng, ctx, 64, 64)
+        cache = make_cache(rng, pages, 2, 64, 128)
+        q, k, v = (torch.tensor(rng.standard_normal((b, n, h, 128))).to(dt).cuda() for h in (8, 2, 2))
+        args = (q, k, v, torch.tensor(tree_masks(rng, b, n)).cuda(), i32(ctx), i32(table))
+        ws = binding.alloc_workspace(binding.treeflash_tree_attention_workspace_bytes(b, n, 8, 2, 128, 64, 64, dt), q.device)
+        got = []
+        for fill in (0, 255, 127):
+            ws.fill_(fill)
+            got.append(binding.treeflash_tree_attention(*args, **cache, scale=0.1, workspace=ws))
+        for out, lse in got[1:]:
+            assert torch.equal(out, got[0][0]) and torch.equal(lse, got[0][1])
